@@ -319,6 +319,33 @@ int dash_sample(const float* d_logits, int64_t ld, int32_t n_rows, int32_t vocab
                 void* stream);
 
 /*
+ * Truncated sampling: dash_sample over the tokens that top_k, top_p and min_p
+ * keep.  (The paper draws from the whole softmax; this is for serving a policy,
+ * and for rollouts that leave its tail out.)  Order a row's finite logits
+ * descending, equal ones by ascending index, and let w_v = exp((l_v - l_max) / T).
+ * A token is kept iff
+ *   - fewer than top_k tokens come before it in the order (top_k = 0: all),
+ *   - the w of the tokens before it sum to less than top_p times the sum over
+ *     the first top_k (top_p = 1: all), and
+ *   - l_v >= l_max + T ln(min_p) (min_p = 0: all),
+ * so the kept tokens are a prefix of the order and never none.  The token drawn is
+ * argmax over the kept tokens of l_v / T + g_v, with dash_sample's noise and rules
+ * (ties to the smallest v; -1 if no l_v is finite): a draw from the kept tokens'
+ * renormalised softmax, equal to dash_sample's whenever that is kept.  The sums of
+ * the second condition decide as in float64; equal calls give equal tokens.
+ * d_logprob_out (nullable) is the log-probability under the whole softmax(l / T),
+ * as dash_sample gives it: comparable with dash_teacher_forced_logprobs at T = 1,
+ * not normalised over the kept tokens.  Other arguments, outputs and errors as
+ * for dash_sample; DASH_EINVAL if top_k < 0, top_p is outside (0, 1] or min_p
+ * outside [0, 1]; DASH_ENOTSUP if top_k is above 1024 and below vocab, or for more
+ * than 2^21 rows.
+ */
+int dash_sample_truncated(const float* d_logits, int64_t ld, int32_t n_rows, int32_t vocab, const int32_t* d_row_of,
+                          const int32_t* d_seq_uid, const int32_t* d_step, float temperature, int32_t top_k,
+                          double top_p, double min_p, uint64_t seed, int32_t* d_tokens_out, float* d_logprob_out,
+                          uint32_t* d_status, void* stream);
+
+/*
  * Self-check of the sampler's screening.  dash_sample first scores every entry
  * with a cheap noise (hardware logarithm) and computes the exact noise only for
  * entries that can still win; this is exact provided the cheap noise is within
@@ -429,6 +456,71 @@ int dash_pg_loss(const float* d_logprobs, int64_t ld, int32_t T, const int32_t* 
  */
 int dash_logits_kl(const float* d_theta, const float* d_base, int64_t ld, int32_t rows, int32_t vocab, float* d_kl,
                    float* d_kl_rev, void* stream);
+
+/* ---- distillation from a teacher's largest logits -------------------------- */
+
+/*
+ * The k largest logits of every row: what a teacher's row is reduced to for
+ * dash_distill_loss (at 151,936 tokens and k = 64, 516 bytes instead of 608 KB), and
+ * the alternatives beside a drawn token.  d_logits: float32 [rows, ld] (ld >= vocab).
+ * d_values [rows, k]: the k largest finite logits, descending, equal ones by ascending
+ * index; d_indices int32 [rows, k]: their tokens.  Rows with fewer than k finite
+ * logits end in -inf and -1.  d_rest float32 [rows] (nullable): ln of the sum of
+ * exp(l_v / T) over the row's other finite logits (-inf if there are none).
+ * DASH_EINVAL if k < 1, temperature <= 0 or not finite, vocab < 1 or > 2^28, or
+ * ld < vocab; DASH_ENOTSUP if k > 1024 or for more than 2^21 rows.
+ */
+int dash_top_logits(const float* d_logits, int64_t ld, int32_t rows, int32_t vocab, int32_t k, float temperature,
+                    float* d_values, int32_t* d_indices, float* d_rest, void* stream);
+
+/*
+ * Distillation loss of student logits against a teacher's k largest logits, per row,
+ * and its gradient: the KL term of Sec. 3.2 (D_KL of the original model against the
+ * policy) from what dash_top_logits keeps of the original model's rows, in a
+ * form that is exact in the kept tokens and treats all others as one outcome.
+ *   p_i     = exp(t_i / T) / P for the teacher's tokens i, p_rest = exp(rest) / P,
+ *             P = sum_i exp(t_i / T) + exp(rest)
+ *   q       = softmax(s / T) of the student, q_rest = its mass on all other tokens
+ *   loss[r] = sum_i p_i ln(p_i / q_i) + p_rest ln(p_rest / q_rest)
+ *   dloss/ds_j = (q_j - p_j) / T for a teacher's token,
+ *                (q_rest - p_rest) (q_j / q_rest) / T for any other.
+ * d_logits: float32 student logits [rows, ld].  d_t_values float32 and d_t_indices
+ * int32 [rows, k], in any order; an index outside [0, vocab) is no entry (padding).
+ * An index may occur once in a row; a row in which one occurs twice gives NaN.
+ * d_t_rest float32 [rows] as dash_top_logits writes it at the same T; NULL means
+ * -inf: the teacher's entries renormalised over themselves.  A teacher without any mass
+ * gives loss 0 and a zero gradient.  A -inf student logit has probability zero (loss
+ * +inf where the teacher gives it mass); a student row with NaN, +inf or
+ * no finite logit gives NaN.  Sums are float32 terms in float64 and float64 for the teacher's
+ * tokens; results do not depend on scheduling.
+ * d_norm float32 [rows, 4]: normalisers of the row, for dash_distill_grad with the same
+ * logits, teacher and T.
+ * DASH_EINVAL and DASH_ENOTSUP as for dash_top_logits.
+ */
+int dash_distill_loss(const float* d_logits, int64_t ld, int32_t rows, int32_t vocab, const float* d_t_values,
+                      const int32_t* d_t_indices, const float* d_t_rest, int32_t k, float temperature, float* d_loss,
+                      float* d_norm, void* stream);
+
+/*
+ * Gradient: d_grad [rows, ld_grad] (ld_grad >= vocab; entries past vocab are left as they
+ * are), of grad_dtype (DASH_F32 or DASH_BF16), = d_weight[r] dloss[r]/ds.  d_weight
+ * float32 [rows] (NULL: 1).  A row of weight 0 (a padded position) gets zeros
+ * whatever its logits, which are not read.  d_grad may be d_logits itself (DASH_F32 and
+ * ld_grad == ld); any other overlap is DASH_EINVAL.
+ */
+int dash_distill_grad(const float* d_logits, int64_t ld, int32_t rows, int32_t vocab, const float* d_t_values,
+                      const int32_t* d_t_indices, const float* d_t_rest, int32_t k, float temperature,
+                      const float* d_norm, const float* d_weight, void* d_grad, int64_t ld_grad, int32_t grad_dtype,
+                      void* stream);
+
+/*
+ * Loss and gradient in one call, for weights that are known before the loss.  As
+ * dash_distill_loss followed by dash_distill_grad, but a row of weight 0 gets loss 0.
+ */
+int dash_distill_loss_grad(const float* d_logits, int64_t ld, int32_t rows, int32_t vocab, const float* d_t_values,
+                           const int32_t* d_t_indices, const float* d_t_rest, int32_t k, float temperature,
+                           const float* d_weight, float* d_loss, void* d_grad, int64_t ld_grad, int32_t grad_dtype,
+                           void* stream);
 
 /*
  * Teacher-forced KL along sampled completions: for every completion position of

@@ -65,6 +65,15 @@ _SIGS = {
                                            _P, C.c_size_t, _P]),
     "dash_sample": (C.c_int, [_P, C.c_int64, C.c_int32, C.c_int32, _P, _P, _P, C.c_float, C.c_uint64, _P, _P, _P,
                               _P, _P]),
+    "dash_sample_truncated": (C.c_int, [_P, C.c_int64, C.c_int32, C.c_int32, _P, _P, _P, C.c_float, C.c_int32,
+                                        C.c_double, C.c_double, C.c_uint64, _P, _P, _P, _P]),
+    "dash_top_logits": (C.c_int, [_P, C.c_int64, C.c_int32, C.c_int32, C.c_int32, C.c_float, _P, _P, _P, _P]),
+    "dash_distill_loss": (C.c_int, [_P, C.c_int64, C.c_int32, C.c_int32, _P, _P, _P, C.c_int32, C.c_float, _P, _P,
+                                    _P]),
+    "dash_distill_grad": (C.c_int, [_P, C.c_int64, C.c_int32, C.c_int32, _P, _P, _P, C.c_int32, C.c_float, _P, _P,
+                                    _P, C.c_int64, C.c_int32, _P]),
+    "dash_distill_loss_grad": (C.c_int, [_P, C.c_int64, C.c_int32, C.c_int32, _P, _P, _P, C.c_int32, C.c_float, _P,
+                                         _P, _P, C.c_int64, C.c_int32, _P]),
     "dash_sampler_check": (C.c_int, [C.POINTER(C.c_double), C.POINTER(C.c_double)]),
     "dash_bf16_round_check": (C.c_int, [C.POINTER(C.c_uint64)]),
     "dash_group_advantage_filter": (C.c_int, [_P, C.c_int32, C.c_int32, C.c_int32, C.c_float, C.c_float, _P, _P,
@@ -233,6 +242,34 @@ def dash_sample(d_logits, ld, n_rows, vocab, d_row_of, d_seq_uid, d_step, temper
                 d_logprob_out, d_row_max_lse, d_status, stream):
     _call("dash_sample", d_logits, ld, n_rows, vocab, d_row_of, d_seq_uid, d_step, C.c_float(temperature),
           C.c_uint64(seed), d_tokens_out, d_logprob_out, d_row_max_lse, d_status, stream)
+
+
+def dash_sample_truncated(d_logits, ld, n_rows, vocab, d_row_of, d_seq_uid, d_step, temperature, top_k, top_p, min_p,
+                          seed, d_tokens_out, d_logprob_out, d_status, stream):
+    _call("dash_sample_truncated", d_logits, ld, n_rows, vocab, d_row_of, d_seq_uid, d_step, C.c_float(temperature),
+          top_k, C.c_double(top_p), C.c_double(min_p), C.c_uint64(seed), d_tokens_out, d_logprob_out, d_status, stream)
+
+
+def dash_top_logits(d_logits, ld, rows, vocab, k, temperature, d_values, d_indices, d_rest, stream):
+    _call("dash_top_logits", d_logits, ld, rows, vocab, k, C.c_float(temperature), d_values, d_indices, d_rest, stream)
+
+
+def dash_distill_loss(d_logits, ld, rows, vocab, d_t_values, d_t_indices, d_t_rest, k, temperature, d_loss, d_norm,
+                      stream):
+    _call("dash_distill_loss", d_logits, ld, rows, vocab, d_t_values, d_t_indices, d_t_rest, k, C.c_float(temperature),
+          d_loss, d_norm, stream)
+
+
+def dash_distill_grad(d_logits, ld, rows, vocab, d_t_values, d_t_indices, d_t_rest, k, temperature, d_norm, d_weight,
+                      d_grad, ld_grad, grad_dtype, stream):
+    _call("dash_distill_grad", d_logits, ld, rows, vocab, d_t_values, d_t_indices, d_t_rest, k, C.c_float(temperature),
+          d_norm, d_weight, d_grad, ld_grad, grad_dtype, stream)
+
+
+def dash_distill_loss_grad(d_logits, ld, rows, vocab, d_t_values, d_t_indices, d_t_rest, k, temperature, d_weight,
+                           d_loss, d_grad, ld_grad, grad_dtype, stream):
+    _call("dash_distill_loss_grad", d_logits, ld, rows, vocab, d_t_values, d_t_indices, d_t_rest, k,
+          C.c_float(temperature), d_weight, d_loss, d_grad, ld_grad, grad_dtype, stream)
 
 
 def dash_group_advantage_filter(d_rewards, n_groups, group, mode, eps, tau, d_adv, d_kept_idx, d_kept_count, stream):

@@ -6,7 +6,7 @@ this file, the native benchmark (csrc/native_bench.hip, a C-ABI client that need
 no Python) into dash_native_bench, and the projection-GEMM micro-benchmark
 (csrc/gemm_bench.hip) into dash_gemm_bench beside it.  The sampler and advantage
 kernels are built with -ffp-contract=off: their float32 arithmetic is part of a
-bit-exact contract.
+bit-exact contract (and so are the operators on rows of logits, which share their headers).
 """
 from __future__ import annotations
 
@@ -24,8 +24,9 @@ NATIVE_BENCH = os.path.join(HERE, "dash_native_bench")
 GEMM_BENCH = os.path.join(HERE, "dash_gemm_bench")
 BUILD = os.path.join(ROOT, "_build")
 
-SOURCES = ["runtime.hip", "elementwise.hip", "gemm.hip", "attention.hip", "sampler.hip", "advantage.hip"]
-EXACT = {"sampler.hip", "advantage.hip"}
+SOURCES = ["runtime.hip", "elementwise.hip", "gemm.hip", "attention.hip", "sampler.hip", "top_logits.hip",
+           "truncate.hip", "distill.hip", "advantage.hip"]
+EXACT = {"sampler.hip", "top_logits.hip", "truncate.hip", "distill.hip", "advantage.hip"}
 
 COMMON = ["--offload-arch=gfx950", "-O3", "-fPIC", "-std=c++17", "-Wall", "-Wno-unused-function",
           "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",

@@ -882,6 +882,34 @@ int scratch_address(void** out) {
     return DASH_OK;
 }
 
+// Arguments common to the operators on rows of logits.
+int check_rows(const char* name, int64_t ld, int32_t rows, int32_t vocab, float temperature) {
+    if (rows < 0 || vocab < 1 || vocab > (1 << 28) || ld < vocab) return fail(DASH_EINVAL, "%s: bad sizes", name);
+    if (!(temperature > 0.f) || !std::isfinite(temperature))
+        return fail(DASH_EINVAL, "%s: temperature must be > 0 and finite", name);
+    if (rows > (1 << 21)) return fail(DASH_ENOTSUP, "%s: more than 2^21 rows", name);  // threads of one launch
+    return DASH_OK;
+}
+
+int check_distill(const char* name, int64_t ld, int32_t rows, int32_t vocab, int32_t k, float temperature) {
+    if (int rc = check_rows(name, ld, rows, vocab, temperature)) return rc;
+    if (k < 1) return fail(DASH_EINVAL, "%s: k must be >= 1", name);
+    if (k > top_logits_max()) return fail(DASH_ENOTSUP, "%s: k %d is above %d", name, k, top_logits_max());
+    return DASH_OK;
+}
+
+// The gradient lies over the logits exactly (float32, the same rows) or not at all.
+int check_grad(const char* name, const float* logits, int64_t ld, int32_t rows, int32_t vocab, const void* grad,
+               int64_t ld_grad, int32_t dtype) {
+    if (dtype != DASH_F32 && dtype != DASH_BF16) return fail(DASH_EINVAL, "%s: bad gradient dtype %d", name, dtype);
+    if (ld_grad < vocab) return fail(DASH_EINVAL, "%s: bad sizes", name);
+    if (rows == 0 || (dtype == DASH_F32 && grad == (const void*)logits && ld_grad == ld)) return DASH_OK;
+    const uintptr_t size = dtype == DASH_F32 ? 4 : 2, l0 = (uintptr_t)logits, g0 = (uintptr_t)grad;
+    const uintptr_t l1 = l0 + 4 * ((uintptr_t)(rows - 1) * ld + vocab), g1 = g0 + size * ((uintptr_t)(rows - 1) * ld_grad + vocab);
+    if (g0 < l1 && l0 < g1) return fail(DASH_EINVAL, "%s: the gradient overlaps the logits", name);
+    return DASH_OK;
+}
+
 }  // namespace
 
 extern "C" {
@@ -931,6 +959,86 @@ int dash_sample(const float* logits, int64_t ld, int32_t rows, int32_t vocab, co
     ProfScope ps(DASH_K_SAMPLE, (hipStream_t)stream);
     DASH_HIP(launch_sample(logits, ld, rows, vocab, row_of, uid, step, temperature, seed, tok_out, lp_out, row_max_lse,
                            d_status, nullptr, nullptr, 0, (hipStream_t)stream));
+    return DASH_OK;
+}
+
+int dash_sample_truncated(const float* logits, int64_t ld, int32_t rows, int32_t vocab, const int32_t* row_of,
+                          const int32_t* uid, const int32_t* step, float temperature, int32_t top_k, double top_p,
+                          double min_p, uint64_t seed, int32_t* tok_out, float* lp_out, uint32_t* d_status,
+                          void* stream) {
+    if (!logits || !uid || !step || !tok_out) return fail(DASH_EINVAL, "dash_sample_truncated: NULL argument");
+    if (int rc = check_rows("dash_sample_truncated", ld, rows, vocab, temperature)) return rc;
+    if (top_k < 0) return fail(DASH_EINVAL, "top_k must be >= 0 (0: all tokens)");
+    if (!(top_p > 0.0 && top_p <= 1.0)) return fail(DASH_EINVAL, "top_p must lie in (0, 1]");
+    if (!(min_p >= 0.0 && min_p <= 1.0)) return fail(DASH_EINVAL, "min_p must lie in [0, 1]");
+    if (top_k > top_logits_max() && top_k < vocab)
+        return fail(DASH_ENOTSUP, "top_k %d is above %d", top_k, top_logits_max());
+    if (rows == 0) return DASH_OK;
+    ProfScope ps(DASH_K_SAMPLE, (hipStream_t)stream);
+    DASH_HIP(launch_sample_truncated(logits, ld, rows, vocab, row_of, uid, step, temperature, top_k, top_p, min_p, seed,
+                                     tok_out, lp_out, d_status, (hipStream_t)stream));
+    return DASH_OK;
+}
+
+int dash_top_logits(const float* logits, int64_t ld, int32_t rows, int32_t vocab, int32_t k, float temperature,
+                    float* d_values, int32_t* d_indices, float* d_rest, void* stream) {
+    if (!logits || !d_values || !d_indices) return fail(DASH_EINVAL, "dash_top_logits: NULL argument");
+    if (int rc = check_rows("dash_top_logits", ld, rows, vocab, temperature)) return rc;
+    if (k < 1) return fail(DASH_EINVAL, "dash_top_logits: k must be >= 1");
+    if (k > top_logits_max()) return fail(DASH_ENOTSUP, "k %d is above %d", k, top_logits_max());
+    if (rows == 0) return DASH_OK;
+    DASH_HIP(launch_top_logits(logits, ld, rows, vocab, k, temperature, d_values, d_indices, d_rest,
+                               (hipStream_t)stream));
+    return DASH_OK;
+}
+
+int dash_distill_loss(const float* logits, int64_t ld, int32_t rows, int32_t vocab, const float* t_values,
+                      const int32_t* t_indices, const float* t_rest, int32_t k, float temperature, float* d_loss,
+                      float* d_norm, void* stream) {
+    if (!logits || !t_values || !t_indices || !d_loss || !d_norm)
+        return fail(DASH_EINVAL, "dash_distill_loss: NULL argument");
+    if (int rc = check_distill("dash_distill_loss", ld, rows, vocab, k, temperature)) return rc;
+    if (rows == 0) return DASH_OK;
+    DistillArgs a{logits, ld, rows, vocab, t_values, t_indices, t_rest, k, temperature};
+    a.loss = d_loss;
+    a.norm = d_norm;
+    DASH_HIP(launch_distill_loss(a, (hipStream_t)stream));
+    return DASH_OK;
+}
+
+int dash_distill_grad(const float* logits, int64_t ld, int32_t rows, int32_t vocab, const float* t_values,
+                      const int32_t* t_indices, const float* t_rest, int32_t k, float temperature,
+                      const float* d_norm, const float* d_weight, void* d_grad, int64_t ld_grad, int32_t grad_dtype,
+                      void* stream) {
+    if (!logits || !t_values || !t_indices || !d_norm || !d_grad)
+        return fail(DASH_EINVAL, "dash_distill_grad: NULL argument");
+    if (int rc = check_distill("dash_distill_grad", ld, rows, vocab, k, temperature)) return rc;
+    if (int rc = check_grad("dash_distill_grad", logits, ld, rows, vocab, d_grad, ld_grad, grad_dtype)) return rc;
+    if (rows == 0) return DASH_OK;
+    DistillArgs a{logits, ld, rows, vocab, t_values, t_indices, t_rest, k, temperature, d_weight};
+    a.norm = const_cast<float*>(d_norm);  // read only where no loss is asked for
+    a.grad = d_grad;
+    a.ld_grad = ld_grad;
+    a.grad_bf16 = grad_dtype == DASH_BF16;
+    DASH_HIP(launch_distill_grad(a, (hipStream_t)stream));
+    return DASH_OK;
+}
+
+int dash_distill_loss_grad(const float* logits, int64_t ld, int32_t rows, int32_t vocab, const float* t_values,
+                           const int32_t* t_indices, const float* t_rest, int32_t k, float temperature,
+                           const float* d_weight, float* d_loss, void* d_grad, int64_t ld_grad, int32_t grad_dtype,
+                           void* stream) {
+    if (!logits || !t_values || !t_indices || !d_loss || !d_grad)
+        return fail(DASH_EINVAL, "dash_distill_loss_grad: NULL argument");
+    if (int rc = check_distill("dash_distill_loss_grad", ld, rows, vocab, k, temperature)) return rc;
+    if (int rc = check_grad("dash_distill_loss_grad", logits, ld, rows, vocab, d_grad, ld_grad, grad_dtype)) return rc;
+    if (rows == 0) return DASH_OK;
+    DistillArgs a{logits, ld, rows, vocab, t_values, t_indices, t_rest, k, temperature, d_weight};
+    a.loss = d_loss;
+    a.grad = d_grad;
+    a.ld_grad = ld_grad;
+    a.grad_bf16 = grad_dtype == DASH_BF16;
+    DASH_HIP(launch_distill_grad(a, (hipStream_t)stream));
     return DASH_OK;
 }
 

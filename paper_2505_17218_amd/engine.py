@@ -160,6 +160,124 @@ def sample(logits: torch.Tensor, seq_uid: torch.Tensor, step: torch.Tensor, temp
     return toks, lps
 
 
+def _check_rows(logits: torch.Tensor, **rows) -> None:
+    """float32 logits [rows, vocab] on a GPU with unit column stride, and tensors of one value (or k) per row beside
+    them: name=(tensor or None, dtype, shape).  The kernels run on the current device and stream."""
+    if logits.dim() != 2 or logits.dtype != torch.float32 or not logits.is_cuda:
+        raise ValueError("logits must be a float32 [rows, vocab] tensor on the GPU")
+    if logits.shape[1] < 1 or (logits.shape[1] > 1 and logits.stride(1) != 1) or \
+            (logits.shape[0] > 1 and logits.stride(0) < logits.shape[1]):
+        raise ValueError("logits need unit column stride and rows that do not overlap")
+    if logits.device.index != torch.cuda.current_device():
+        raise ValueError(f"logits are on {logits.device}, the current device is cuda:{torch.cuda.current_device()}")
+    for name, (t, dtype, shape) in rows.items():
+        if t is None:
+            continue
+        if t.device != logits.device or t.dtype != dtype or tuple(t.shape) != shape or not t.is_contiguous():
+            raise ValueError(f"{name} must be a contiguous {dtype} tensor of shape {shape} on {logits.device}")
+
+
+def _ld(t: torch.Tensor) -> int:
+    return t.stride(0) if t.shape[0] > 1 else t.shape[1]
+
+
+def sample_truncated(logits: torch.Tensor, seq_uid: torch.Tensor, step: torch.Tensor, temperature: float, seed: int,
+                     top_k: int = 0, top_p: float = 1.0, min_p: float = 0.0, row_of: torch.Tensor | None = None,
+                     with_logprob: bool = True, status: torch.Tensor | None = None):
+    """dash_sample_truncated: (int32 tokens [n], float32 log-probs [n] under the whole softmax, or None), one per
+    seq_uid.  top_k 0, top_p 1 and min_p 0 each keep every token.  row_of int32 [n]: the logits row of each draw,
+    which must lie in [0, rows) (it is not checked); status int32 [1] (bits OR-ed in)."""
+    n = seq_uid.numel()
+    _check_rows(logits, seq_uid=(seq_uid, torch.int32, (n,)), step=(step, torch.int32, (n,)),
+                row_of=(row_of, torch.int32, (n,)), status=(status, torch.int32, (1,)))
+    if row_of is None and n > logits.shape[0]:
+        raise ValueError(f"{n} draws from {logits.shape[0]} rows of logits")
+    toks = torch.empty(n, dtype=torch.int32, device=logits.device)
+    lps = torch.empty(n, dtype=torch.float32, device=logits.device) if with_logprob else None
+    if n:
+        L.dash_sample_truncated(logits.data_ptr(), _ld(logits), n, logits.shape[1], L.ptr(row_of), seq_uid.data_ptr(),
+                                step.data_ptr(), temperature, top_k, top_p, min_p, seed, toks.data_ptr(), L.ptr(lps),
+                                L.ptr(status), stream_handle())
+    return toks, lps
+
+
+def top_logits(logits: torch.Tensor, k: int, temperature: float = 1.0):
+    """dash_top_logits: (float32 values [rows, k], int32 indices [rows, k], float32 rest [rows]): the k largest logits
+    of every row and the log-sum-exp of all others at the temperature."""
+    _check_rows(logits)
+    rows, V = logits.shape
+    values = torch.empty(rows, max(k, 0), dtype=torch.float32, device=logits.device)
+    indices = torch.empty(rows, max(k, 0), dtype=torch.int32, device=logits.device)
+    rest = torch.empty(rows, dtype=torch.float32, device=logits.device)
+    if rows:
+        L.dash_top_logits(logits.data_ptr(), _ld(logits), rows, V, k, temperature, values.data_ptr(),
+                          indices.data_ptr(), rest.data_ptr(), stream_handle())
+    return values, indices, rest
+
+
+def _check_distill(logits, values, indices, rest, norm=None, weight=None):
+    rows = logits.shape[0]
+    if values.dim() != 2:
+        raise ValueError("the teacher's values must be [rows, k]")
+    k = values.shape[1]
+    _check_rows(logits, values=(values, torch.float32, (rows, k)), indices=(indices, torch.int32, (rows, k)),
+                rest=(rest, torch.float32, (rows,)), norm=(norm, torch.float32, (rows, 4)),
+                weight=(weight, torch.float32, (rows,)))
+    return rows, logits.shape[1], k
+
+
+def _grad_buffer(logits: torch.Tensor, out: torch.Tensor | None, dtype: torch.dtype):
+    if out is None:
+        out = torch.empty(logits.shape, dtype=dtype, device=logits.device)
+    if out.dtype not in (torch.float32, torch.bfloat16) or out.shape != logits.shape or out.device != logits.device or \
+            (out.shape[1] > 1 and out.stride(1) != 1) or (out.shape[0] > 1 and out.stride(0) < out.shape[1]):
+        raise ValueError("the gradient must be float32 or bfloat16, of the logits' shape and device, with unit column "
+                         "stride")
+    return out, L.DASH_BF16 if out.dtype == torch.bfloat16 else L.DASH_F32
+
+
+def distill_loss(logits: torch.Tensor, values: torch.Tensor, indices: torch.Tensor, rest: torch.Tensor | None = None,
+                 temperature: float = 1.0):
+    """dash_distill_loss against a teacher's entries as top_logits gives them (rest None: renormalised over the
+    entries): (float32 loss [rows], float32 normalisers [rows, 4] for distill_grad)."""
+    rows, V, k = _check_distill(logits, values, indices, rest)
+    loss = torch.empty(rows, dtype=torch.float32, device=logits.device)
+    norm = torch.empty(rows, 4, dtype=torch.float32, device=logits.device)
+    if rows:
+        L.dash_distill_loss(logits.data_ptr(), _ld(logits), rows, V, values.data_ptr(), indices.data_ptr(),
+                            L.ptr(rest), k, temperature, loss.data_ptr(), norm.data_ptr(), stream_handle())
+    return loss, norm
+
+
+def distill_grad(logits: torch.Tensor, values: torch.Tensor, indices: torch.Tensor, norm: torch.Tensor,
+                 rest: torch.Tensor | None = None, temperature: float = 1.0, weight: torch.Tensor | None = None,
+                 out: torch.Tensor | None = None, dtype: torch.dtype = torch.float32) -> torch.Tensor:
+    """dash_distill_grad: weight[r] dloss[r]/dlogits [rows, vocab] (weight None: 1), into out (which may be the logits)
+    or a new tensor of dtype float32 or bfloat16."""
+    rows, V, k = _check_distill(logits, values, indices, rest, norm, weight)
+    out, code = _grad_buffer(logits, out, dtype)
+    if rows:
+        L.dash_distill_grad(logits.data_ptr(), _ld(logits), rows, V, values.data_ptr(), indices.data_ptr(),
+                            L.ptr(rest), k, temperature, norm.data_ptr(), L.ptr(weight), out.data_ptr(), _ld(out), code,
+                            stream_handle())
+    return out
+
+
+def distill_loss_grad(logits: torch.Tensor, values: torch.Tensor, indices: torch.Tensor,
+                      rest: torch.Tensor | None = None, temperature: float = 1.0, weight: torch.Tensor | None = None,
+                      out: torch.Tensor | None = None, dtype: torch.dtype = torch.float32):
+    """dash_distill_loss_grad: (loss [rows], gradient [rows, vocab]) in one call; a row of weight 0 gets loss 0 and a
+    zero gradient."""
+    rows, V, k = _check_distill(logits, values, indices, rest, weight=weight)
+    out, code = _grad_buffer(logits, out, dtype)
+    loss = torch.empty(rows, dtype=torch.float32, device=logits.device)
+    if rows:
+        L.dash_distill_loss_grad(logits.data_ptr(), _ld(logits), rows, V, values.data_ptr(), indices.data_ptr(),
+                                 L.ptr(rest), k, temperature, L.ptr(weight), loss.data_ptr(), out.data_ptr(), _ld(out),
+                                 code, stream_handle())
+    return loss, out
+
+
 def advantage_filter(rewards: torch.Tensor, group: int, mode: int = L.DASH_ADV_STD_SAMPLE, eps: float = 1e-6,
                      tau: float = 0.1):
     """dash_group_advantage_filter: returns (float32 A [N], int32 kept indices [K] on the device)."""
