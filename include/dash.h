@@ -338,12 +338,16 @@ int dash_sample(const float* d_logits, int64_t ld, int32_t n_rows, int32_t vocab
  * not normalised over the kept tokens.  Other arguments, outputs and errors as
  * for dash_sample; DASH_EINVAL if top_k < 0, top_p is outside (0, 1] or min_p
  * outside [0, 1]; DASH_ENOTSUP if top_k is above 1024 and below vocab, or for more
- * than 2^21 rows.
+ * than 2^21 rows.  d_ws: dash_sample_truncated_workspace_bytes(n_rows, vocab, top_k)
+ * bytes, 256-byte aligned (as every workspace here; may be NULL where that is 0), of which
+ * nothing has to be cleared or kept; calls that may overlap in time, and graphs that may
+ * be replayed at the same time, need one each.  DASH_ECAPACITY if it is too small.
  */
+size_t dash_sample_truncated_workspace_bytes(int32_t n_rows, int32_t vocab, int32_t top_k);
 int dash_sample_truncated(const float* d_logits, int64_t ld, int32_t n_rows, int32_t vocab, const int32_t* d_row_of,
                           const int32_t* d_seq_uid, const int32_t* d_step, float temperature, int32_t top_k,
                           double top_p, double min_p, uint64_t seed, int32_t* d_tokens_out, float* d_logprob_out,
-                          uint32_t* d_status, void* stream);
+                          uint32_t* d_status, void* d_ws, size_t ws_bytes, void* stream);
 
 /*
  * Self-check of the sampler's screening.  dash_sample first scores every entry
@@ -468,10 +472,12 @@ int dash_logits_kl(const float* d_theta, const float* d_base, int64_t ld, int32_
  * logits end in -inf and -1.  d_rest float32 [rows] (nullable): ln of the sum of
  * exp(l_v / T) over the row's other finite logits (-inf if there are none).
  * DASH_EINVAL if k < 1, temperature <= 0 or not finite, vocab < 1 or > 2^28, or
- * ld < vocab; DASH_ENOTSUP if k > 1024 or for more than 2^21 rows.
+ * ld < vocab; DASH_ENOTSUP if k > 1024 or for more than 2^21 rows.  d_ws as for
+ * dash_sample_truncated, dash_top_logits_workspace_bytes(rows, vocab, k) bytes.
  */
+size_t dash_top_logits_workspace_bytes(int32_t rows, int32_t vocab, int32_t k);
 int dash_top_logits(const float* d_logits, int64_t ld, int32_t rows, int32_t vocab, int32_t k, float temperature,
-                    float* d_values, int32_t* d_indices, float* d_rest, void* stream);
+                    float* d_values, int32_t* d_indices, float* d_rest, void* d_ws, size_t ws_bytes, void* stream);
 
 /*
  * Distillation loss of student logits against a teacher's k largest logits, per row,
@@ -495,11 +501,13 @@ int dash_top_logits(const float* d_logits, int64_t ld, int32_t rows, int32_t voc
  * tokens; results do not depend on scheduling.
  * d_norm float32 [rows, 4]: normalisers of the row, for dash_distill_grad with the same
  * logits, teacher and T.
- * DASH_EINVAL and DASH_ENOTSUP as for dash_top_logits.
+ * DASH_EINVAL and DASH_ENOTSUP as for dash_top_logits.  d_ws as for dash_sample_truncated,
+ * dash_distill_workspace_bytes(rows, vocab) bytes.
  */
+size_t dash_distill_workspace_bytes(int32_t rows, int32_t vocab);
 int dash_distill_loss(const float* d_logits, int64_t ld, int32_t rows, int32_t vocab, const float* d_t_values,
                       const int32_t* d_t_indices, const float* d_t_rest, int32_t k, float temperature, float* d_loss,
-                      float* d_norm, void* stream);
+                      float* d_norm, void* d_ws, size_t ws_bytes, void* stream);
 
 /*
  * Gradient: d_grad [rows, ld_grad] (ld_grad >= vocab; entries past vocab are left as they
@@ -516,11 +524,12 @@ int dash_distill_grad(const float* d_logits, int64_t ld, int32_t rows, int32_t v
 /*
  * Loss and gradient in one call, for weights that are known before the loss.  As
  * dash_distill_loss followed by dash_distill_grad, but a row of weight 0 gets loss 0.
+ * d_ws: dash_distill_workspace_bytes(rows, vocab) bytes.
  */
 int dash_distill_loss_grad(const float* d_logits, int64_t ld, int32_t rows, int32_t vocab, const float* d_t_values,
                            const int32_t* d_t_indices, const float* d_t_rest, int32_t k, float temperature,
                            const float* d_weight, float* d_loss, void* d_grad, int64_t ld_grad, int32_t grad_dtype,
-                           void* stream);
+                           void* d_ws, size_t ws_bytes, void* stream);
 
 /*
  * Teacher-forced KL along sampled completions: for every completion position of

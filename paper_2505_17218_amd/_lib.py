@@ -66,14 +66,18 @@ _SIGS = {
     "dash_sample": (C.c_int, [_P, C.c_int64, C.c_int32, C.c_int32, _P, _P, _P, C.c_float, C.c_uint64, _P, _P, _P,
                               _P, _P]),
     "dash_sample_truncated": (C.c_int, [_P, C.c_int64, C.c_int32, C.c_int32, _P, _P, _P, C.c_float, C.c_int32,
-                                        C.c_double, C.c_double, C.c_uint64, _P, _P, _P, _P]),
-    "dash_top_logits": (C.c_int, [_P, C.c_int64, C.c_int32, C.c_int32, C.c_int32, C.c_float, _P, _P, _P, _P]),
+                                        C.c_double, C.c_double, C.c_uint64, _P, _P, _P, _P, C.c_size_t, _P]),
+    "dash_sample_truncated_workspace_bytes": (C.c_size_t, [C.c_int32, C.c_int32, C.c_int32]),
+    "dash_top_logits_workspace_bytes": (C.c_size_t, [C.c_int32, C.c_int32, C.c_int32]),
+    "dash_top_logits": (C.c_int, [_P, C.c_int64, C.c_int32, C.c_int32, C.c_int32, C.c_float, _P, _P, _P, _P,
+                                  C.c_size_t, _P]),
+    "dash_distill_workspace_bytes": (C.c_size_t, [C.c_int32, C.c_int32]),
     "dash_distill_loss": (C.c_int, [_P, C.c_int64, C.c_int32, C.c_int32, _P, _P, _P, C.c_int32, C.c_float, _P, _P,
-                                    _P]),
+                                    _P, C.c_size_t, _P]),
     "dash_distill_grad": (C.c_int, [_P, C.c_int64, C.c_int32, C.c_int32, _P, _P, _P, C.c_int32, C.c_float, _P, _P,
                                     _P, C.c_int64, C.c_int32, _P]),
     "dash_distill_loss_grad": (C.c_int, [_P, C.c_int64, C.c_int32, C.c_int32, _P, _P, _P, C.c_int32, C.c_float, _P,
-                                         _P, _P, C.c_int64, C.c_int32, _P]),
+                                         _P, _P, C.c_int64, C.c_int32, _P, C.c_size_t, _P]),
     "dash_sampler_check": (C.c_int, [C.POINTER(C.c_double), C.POINTER(C.c_double)]),
     "dash_bf16_round_check": (C.c_int, [C.POINTER(C.c_uint64)]),
     "dash_group_advantage_filter": (C.c_int, [_P, C.c_int32, C.c_int32, C.c_int32, C.c_float, C.c_float, _P, _P,
@@ -245,19 +249,33 @@ def dash_sample(d_logits, ld, n_rows, vocab, d_row_of, d_seq_uid, d_step, temper
 
 
 def dash_sample_truncated(d_logits, ld, n_rows, vocab, d_row_of, d_seq_uid, d_step, temperature, top_k, top_p, min_p,
-                          seed, d_tokens_out, d_logprob_out, d_status, stream):
+                          seed, d_tokens_out, d_logprob_out, d_status, d_ws, ws_bytes, stream):
     _call("dash_sample_truncated", d_logits, ld, n_rows, vocab, d_row_of, d_seq_uid, d_step, C.c_float(temperature),
-          top_k, C.c_double(top_p), C.c_double(min_p), C.c_uint64(seed), d_tokens_out, d_logprob_out, d_status, stream)
+          top_k, C.c_double(top_p), C.c_double(min_p), C.c_uint64(seed), d_tokens_out, d_logprob_out, d_status,
+          d_ws, ws_bytes, stream)
 
 
-def dash_top_logits(d_logits, ld, rows, vocab, k, temperature, d_values, d_indices, d_rest, stream):
-    _call("dash_top_logits", d_logits, ld, rows, vocab, k, C.c_float(temperature), d_values, d_indices, d_rest, stream)
+def dash_sample_truncated_workspace_bytes(n_rows, vocab, top_k) -> int:
+    return load().dash_sample_truncated_workspace_bytes(n_rows, vocab, top_k)
+
+
+def dash_top_logits_workspace_bytes(rows, vocab, k) -> int:
+    return load().dash_top_logits_workspace_bytes(rows, vocab, k)
+
+
+def dash_top_logits(d_logits, ld, rows, vocab, k, temperature, d_values, d_indices, d_rest, d_ws, ws_bytes, stream):
+    _call("dash_top_logits", d_logits, ld, rows, vocab, k, C.c_float(temperature), d_values, d_indices, d_rest, d_ws,
+          ws_bytes, stream)
+
+
+def dash_distill_workspace_bytes(rows, vocab) -> int:
+    return load().dash_distill_workspace_bytes(rows, vocab)
 
 
 def dash_distill_loss(d_logits, ld, rows, vocab, d_t_values, d_t_indices, d_t_rest, k, temperature, d_loss, d_norm,
-                      stream):
+                      d_ws, ws_bytes, stream):
     _call("dash_distill_loss", d_logits, ld, rows, vocab, d_t_values, d_t_indices, d_t_rest, k, C.c_float(temperature),
-          d_loss, d_norm, stream)
+          d_loss, d_norm, d_ws, ws_bytes, stream)
 
 
 def dash_distill_grad(d_logits, ld, rows, vocab, d_t_values, d_t_indices, d_t_rest, k, temperature, d_norm, d_weight,
@@ -267,9 +285,9 @@ def dash_distill_grad(d_logits, ld, rows, vocab, d_t_values, d_t_indices, d_t_re
 
 
 def dash_distill_loss_grad(d_logits, ld, rows, vocab, d_t_values, d_t_indices, d_t_rest, k, temperature, d_weight,
-                           d_loss, d_grad, ld_grad, grad_dtype, stream):
+                           d_loss, d_grad, ld_grad, grad_dtype, d_ws, ws_bytes, stream):
     _call("dash_distill_loss_grad", d_logits, ld, rows, vocab, d_t_values, d_t_indices, d_t_rest, k,
-          C.c_float(temperature), d_weight, d_loss, d_grad, ld_grad, grad_dtype, stream)
+          C.c_float(temperature), d_weight, d_loss, d_grad, ld_grad, grad_dtype, d_ws, ws_bytes, stream)
 
 
 def dash_group_advantage_filter(d_rewards, n_groups, group, mode, eps, tau, d_adv, d_kept_idx, d_kept_count, stream):

@@ -159,14 +159,16 @@ hipError_t launch_logits_kl(const float* theta, const float* base, int64_t ld, i
 // with their indices; missing ones -inf and -1.  rest (nullable): log of the sum of e^(l / T) over the
 // row's other finite logits.
 int top_logits_max();
+size_t top_workspace_bytes(int rows, int vocab, int k);
 hipError_t launch_top_logits(const float* logits, int64_t ld, int rows, int vocab, int k, float temperature,
-                             float* values, int32_t* indices, float* rest, hipStream_t st);
+                             float* values, int32_t* indices, float* rest, void* ws, hipStream_t st);
 // launch_sample's draw over the tokens that top_k (0: all; at most top_logits_max() where below
 // vocab), top_p in (0, 1] and min_p in [0, 1] keep.  lp_out (nullable): log-prob over all tokens.
+size_t sample_truncated_workspace_bytes(int rows, int vocab, int top_k);
 hipError_t launch_sample_truncated(const float* logits, int64_t ld, int rows, int vocab, const int32_t* row_of,
                                    const int32_t* uid, const int32_t* step, float temperature, int top_k, double top_p,
                                    double min_p, uint64_t seed, int32_t* tok_out, float* lp_out, uint32_t* status,
-                                   hipStream_t st);
+                                   void* ws, hipStream_t st);
 // Distillation from a teacher's k largest logits (distill.hip).
 struct DistillArgs {
     const float* logits;  // student [rows, ld]
@@ -177,7 +179,7 @@ struct DistillArgs {
     const float* t_rest;   // [rows], nullable
     int k;
     float temperature;
-    const float* weight;  // [rows], nullable: 1 (gradients only)
+    const float* weight;  // [rows], nullable: 1; rows of weight 0 have loss 0 and are not read
     float* loss;          // [rows]
     float* norm;          // [rows, 4]: written by the loss, read by the gradient
     void* grad;           // [rows, ld_grad]
@@ -185,9 +187,11 @@ struct DistillArgs {
     int grad_bf16;
     float scale, scale_low;  // filled in by the launchers
 };
-hipError_t launch_distill_loss(DistillArgs a, hipStream_t st);
-// With a.loss: loss and gradient in one launch (a.norm unused); without: the gradient from a.norm.
+size_t distill_workspace_bytes(int rows, int vocab);
+hipError_t launch_distill_loss(DistillArgs a, void* ws, hipStream_t st);
 hipError_t launch_distill_grad(DistillArgs a, hipStream_t st);
+// Both; a.norm is not used.
+hipError_t launch_distill_loss_grad(DistillArgs a, void* ws, hipStream_t st);
 // *loss = -(1/n_total) sum over kept samples n of A[n] * sum_{t < len[n]} lp[n][t] (float64);
 // seq_lp[n] (nullable) receives each kept sample's sequence log-prob.
 hipError_t launch_pg_loss(const float* lp, int64_t ld, int T, const int32_t* len, const float* adv,

@@ -16,20 +16,26 @@ constexpr int kRowTile = 4 * kRowThreads;  // entries of one step: four consecut
 
 // Rows start on any float: gfx950 loads 16 bytes from a 4-byte aligned address in one instruction.
 typedef float f32x4u_t __attribute__((ext_vector_type(4), aligned(4)));
+// (row is the same for the whole work-group: its address stays in scalar registers, and a lane
+// holds a 32-bit offset.)
 template <bool STREAM>
-DASH_DEV f32x4_t load_row4(const float* p) {
-    const f32x4u_t* q = reinterpret_cast<const f32x4u_t*>(p);
+DASH_DEV f32x4_t load_row4(const float* row, int i) {
+    const f32x4u_t* q = reinterpret_cast<const f32x4u_t*>(reinterpret_cast<const char*>(row) + (uint32_t)i * 4u);
     if constexpr (STREAM) return __builtin_nontemporal_load(q);
     else return *q;
 }
 
-// Calls f(l, i) with entries i .. i+3 of row for every group of four in [lo, hi), whole tiles first,
-// in ascending order; entries past hi are -inf.  Every thread of the work-group makes the same
-// number of calls, so f may hold barriers.  DEPTH tiles are in flight: a thread's registers are
-// used, then loaded again DEPTH tiles ahead (past the end: the last tile once more), so no wait
-// covers a load younger than the one that is needed.  STREAM: rows that nothing reads again.
-template <int DEPTH, bool STREAM, class F>
-DASH_DEV void walk_row(const float* __restrict__ row, int lo, int hi, F&& f) {
+// Calls f(l, i) with entries i .. i+3 of row for every group of four in [lo, hi); entries past hi are
+// -inf.  Every thread of the work-group makes the same number of calls, so f may hold barriers.
+// DEPTH tiles are in flight: a thread's registers are used, then loaded again (past the end: with a
+// tile that is in bounds, unused), so no wait covers a load younger than the one that is needed.
+// In order: whole tiles ascending, then the partial one.  STRIPES: the whole tiles as DEPTH stripes
+// side by side, so that the first DEPTH tiles are a sample of the whole row.  start(buf, whole) sees
+// these before f does; where there are fewer whole tiles than DEPTH, the last one (the partial one,
+// if there is none) fills the places of the missing.  round(t) is called after the t-th DEPTH tiles
+// (1, 2, ...) and ends the walk by returning true.  STREAM: rows that nothing reads again.
+template <int DEPTH, bool STRIPES, bool STREAM, class START, class F, class ROUND>
+DASH_DEV void walk_row(const float* __restrict__ row, int lo, int hi, START&& start, F&& f, ROUND&& round) {
     const int whole = (hi - lo) / kRowTile;
     const int end = lo + whole * kRowTile, at = lo + 4 * (int)threadIdx.x;
     f32x4_t last = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
@@ -40,20 +46,51 @@ DASH_DEV void walk_row(const float* __restrict__ row, int lo, int hi, F&& f) {
             if (i + j < hi) last[j] = row[i + j];
     }
     if (whole) {
+        // Round t < rounds is tiles t of the stripes (or the next DEPTH tiles); the round after it, the
+        // left-over tiles.
+        const int rounds = whole / DEPTH, left = whole - rounds * DEPTH;
+        auto tile = [&](int t, int d) {
+            return t >= rounds ? min(rounds * DEPTH + d, whole - 1) : STRIPES ? d * rounds + t : t * DEPTH + d;
+        };
         f32x4_t buf[DEPTH];
 #pragma unroll
-        for (int d = 0; d < DEPTH; ++d) buf[d] = load_row4<STREAM>(row + at + min(d, whole - 1) * kRowTile);
-        for (int t0 = 0; t0 < whole; t0 += DEPTH) {
+        for (int d = 0; d < DEPTH; ++d) buf[d] = load_row4<STREAM>(row, at + tile(0, d) * kRowTile);
+        start(buf, whole);
+        for (int t = 0; t < rounds; ++t) {
 #pragma unroll
             for (int d = 0; d < DEPTH; ++d) {
-                const int t = t0 + d;
-                if (t >= whole) break;
-                f(buf[d], at + t * kRowTile);
-                buf[d] = load_row4<STREAM>(row + at + min(t + DEPTH, whole - 1) * kRowTile);
+                f(buf[d], at + tile(t, d) * kRowTile);
+                buf[d] = load_row4<STREAM>(row, at + tile(t + 1, d) * kRowTile);
             }
+            if (round(t + 1)) return;
         }
+#pragma unroll
+        for (int d = 0; d < DEPTH - 1; ++d) {
+            if (d >= left) break;
+            f(buf[d], at + tile(rounds, d) * kRowTile);
+        }
+    } else {
+        f32x4_t buf[DEPTH];
+#pragma unroll
+        for (int d = 0; d < DEPTH; ++d) buf[d] = last;
+        start(buf, 0);
     }
     if (end < hi) f(last, end + 4 * (int)threadIdx.x);
+}
+template <int DEPTH, bool STREAM, class F>
+DASH_DEV void walk_row(const float* __restrict__ row, int lo, int hi, F&& f) {
+    walk_row<DEPTH, false, STREAM>(row, lo, hi, [](const f32x4_t (&)[DEPTH], int) {}, (F&&)f, [](int) { return false; });
+}
+
+// Rows cut into n stretches of len entries (the last one shorter, none empty; len a multiple of four),
+// each walked by a work-group of its own.
+struct RowSplit {
+    int n, len;
+};
+inline RowSplit split_row(int vocab, int n) {
+    if (n <= 1) return {1, vocab};
+    const int len = ((vocab + n - 1) / n + 3) & ~3;
+    return {(vocab + len - 1) / len, len};
 }
 
 // log2(e) / T, so that e^((x - m) / T) = 2^((x - m) scale); finite for every T > 0 (0 times it stays 0).
@@ -95,6 +132,30 @@ DASH_DEV void exp_push4(ExpSum& s, const f32x4_t& x, float m4, float scale, floa
     s.z += (double)((e[0] + e[1]) + (e[2] + e[3]));
 }
 
+// Inclusive sum over the threads up to this one (of kRowThreads), and the total.
+template <class T>
+DASH_DEV T block_scan(T v, T* red, T& total) {
+    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+        const T u = __shfl_up(v, o, 64);
+        if (lane >= o) v += u;
+    }
+    __syncthreads();
+    if (lane == 63) red[w] = v;
+    __syncthreads();
+    // every wave sums the waves' totals, a lane each
+    T t = lane < kRowWaves ? red[lane] : (T)0;
+#pragma unroll
+    for (int o = 1; o < kRowWaves; o <<= 1) {
+        const T u = __shfl_up(t, o, 64);
+        if (lane >= o) t += u;
+    }
+    total = __shfl(t, kRowWaves - 1, 64);
+    const T before = __shfl(t, max(w - 1, 0), 64);
+    return v + (w ? before : (T)0);
+}
+
 DASH_DEV float max4(const f32x4_t& x) { return fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])); }
 
 // Reductions over the work-group's kRowThreads threads in a fixed order; every thread gets the
@@ -117,6 +178,13 @@ DASH_DEV double block_sum_d(double v, double* red) {
 }
 DASH_DEV float block_max_f(float v, float* red) {
     return block_reduce(v, red, [](float a, float b) { return fmaxf(a, b); });
+}
+
+// Sum over the work-group's threads of e^((l - ref) / T) (0: nothing), and ref.
+DASH_DEV double block_exp_sum(const ExpSum& s, double temperature, float* red_f, double* red_d, float& ref) {
+    ref = block_max_f(s.z > 0.0 ? s.ref : -FLT_MAX, red_f);
+    // (a NaN sum stays one)
+    return block_sum_d(s.z == 0.0 ? 0.0 : s.z * exp(((double)s.ref - (double)ref) / temperature), red_d);
 }
 
 }  // namespace dash

@@ -891,6 +891,13 @@ int check_rows(const char* name, int64_t ld, int32_t rows, int32_t vocab, float 
     return DASH_OK;
 }
 
+int check_room(const char* name, const void* ws, size_t have, size_t need) {
+    if (need && ((uintptr_t)ws & 255)) return fail(DASH_EINVAL, "%s: the workspace must be 256-byte aligned", name);
+    if (have < need || (need && !ws))
+        return fail(DASH_ECAPACITY, "%s: workspace too small: %zu < %zu bytes", name, ws ? have : (size_t)0, need);
+    return DASH_OK;
+}
+
 int check_distill(const char* name, int64_t ld, int32_t rows, int32_t vocab, int32_t k, float temperature) {
     if (int rc = check_rows(name, ld, rows, vocab, temperature)) return rc;
     if (k < 1) return fail(DASH_EINVAL, "%s: k must be >= 1", name);
@@ -962,10 +969,15 @@ int dash_sample(const float* logits, int64_t ld, int32_t rows, int32_t vocab, co
     return DASH_OK;
 }
 
+size_t dash_sample_truncated_workspace_bytes(int32_t rows, int32_t vocab, int32_t top_k) {
+    if (rows < 1 || vocab < 1 || top_k < 0 || (top_k > top_logits_max() && top_k < vocab)) return 0;
+    return sample_truncated_workspace_bytes(rows, vocab, top_k);
+}
+
 int dash_sample_truncated(const float* logits, int64_t ld, int32_t rows, int32_t vocab, const int32_t* row_of,
                           const int32_t* uid, const int32_t* step, float temperature, int32_t top_k, double top_p,
                           double min_p, uint64_t seed, int32_t* tok_out, float* lp_out, uint32_t* d_status,
-                          void* stream) {
+                          void* ws, size_t ws_bytes, void* stream) {
     if (!logits || !uid || !step || !tok_out) return fail(DASH_EINVAL, "dash_sample_truncated: NULL argument");
     if (int rc = check_rows("dash_sample_truncated", ld, rows, vocab, temperature)) return rc;
     if (top_k < 0) return fail(DASH_EINVAL, "top_k must be >= 0 (0: all tokens)");
@@ -974,27 +986,37 @@ int dash_sample_truncated(const float* logits, int64_t ld, int32_t rows, int32_t
     if (top_k > top_logits_max() && top_k < vocab)
         return fail(DASH_ENOTSUP, "top_k %d is above %d", top_k, top_logits_max());
     if (rows == 0) return DASH_OK;
+    if (int rc = check_room("dash_sample_truncated", ws, ws_bytes, sample_truncated_workspace_bytes(rows, vocab, top_k))) return rc;
     ProfScope ps(DASH_K_SAMPLE, (hipStream_t)stream);
     DASH_HIP(launch_sample_truncated(logits, ld, rows, vocab, row_of, uid, step, temperature, top_k, top_p, min_p, seed,
-                                     tok_out, lp_out, d_status, (hipStream_t)stream));
+                                     tok_out, lp_out, d_status, ws, (hipStream_t)stream));
     return DASH_OK;
 }
 
+size_t dash_top_logits_workspace_bytes(int32_t rows, int32_t vocab, int32_t k) {
+    return rows < 1 || vocab < 1 || k < 1 || k > top_logits_max() ? 0 : top_workspace_bytes(rows, vocab, k);
+}
+
 int dash_top_logits(const float* logits, int64_t ld, int32_t rows, int32_t vocab, int32_t k, float temperature,
-                    float* d_values, int32_t* d_indices, float* d_rest, void* stream) {
+                    float* d_values, int32_t* d_indices, float* d_rest, void* ws, size_t ws_bytes, void* stream) {
     if (!logits || !d_values || !d_indices) return fail(DASH_EINVAL, "dash_top_logits: NULL argument");
     if (int rc = check_rows("dash_top_logits", ld, rows, vocab, temperature)) return rc;
     if (k < 1) return fail(DASH_EINVAL, "dash_top_logits: k must be >= 1");
     if (k > top_logits_max()) return fail(DASH_ENOTSUP, "k %d is above %d", k, top_logits_max());
     if (rows == 0) return DASH_OK;
-    DASH_HIP(launch_top_logits(logits, ld, rows, vocab, k, temperature, d_values, d_indices, d_rest,
+    if (int rc = check_room("dash_top_logits", ws, ws_bytes, top_workspace_bytes(rows, vocab, k))) return rc;
+    DASH_HIP(launch_top_logits(logits, ld, rows, vocab, k, temperature, d_values, d_indices, d_rest, ws,
                                (hipStream_t)stream));
     return DASH_OK;
 }
 
+size_t dash_distill_workspace_bytes(int32_t rows, int32_t vocab) {
+    return rows < 1 || vocab < 1 ? 0 : distill_workspace_bytes(rows, vocab);
+}
+
 int dash_distill_loss(const float* logits, int64_t ld, int32_t rows, int32_t vocab, const float* t_values,
                       const int32_t* t_indices, const float* t_rest, int32_t k, float temperature, float* d_loss,
-                      float* d_norm, void* stream) {
+                      float* d_norm, void* ws, size_t ws_bytes, void* stream) {
     if (!logits || !t_values || !t_indices || !d_loss || !d_norm)
         return fail(DASH_EINVAL, "dash_distill_loss: NULL argument");
     if (int rc = check_distill("dash_distill_loss", ld, rows, vocab, k, temperature)) return rc;
@@ -1002,7 +1024,8 @@ int dash_distill_loss(const float* logits, int64_t ld, int32_t rows, int32_t voc
     DistillArgs a{logits, ld, rows, vocab, t_values, t_indices, t_rest, k, temperature};
     a.loss = d_loss;
     a.norm = d_norm;
-    DASH_HIP(launch_distill_loss(a, (hipStream_t)stream));
+    if (int rc = check_room("dash_distill_loss", ws, ws_bytes, distill_workspace_bytes(rows, vocab))) return rc;
+    DASH_HIP(launch_distill_loss(a, ws, (hipStream_t)stream));
     return DASH_OK;
 }
 
@@ -1016,7 +1039,7 @@ int dash_distill_grad(const float* logits, int64_t ld, int32_t rows, int32_t voc
     if (int rc = check_grad("dash_distill_grad", logits, ld, rows, vocab, d_grad, ld_grad, grad_dtype)) return rc;
     if (rows == 0) return DASH_OK;
     DistillArgs a{logits, ld, rows, vocab, t_values, t_indices, t_rest, k, temperature, d_weight};
-    a.norm = const_cast<float*>(d_norm);  // read only where no loss is asked for
+    a.norm = const_cast<float*>(d_norm);  // (the gradient only reads it)
     a.grad = d_grad;
     a.ld_grad = ld_grad;
     a.grad_bf16 = grad_dtype == DASH_BF16;
@@ -1027,7 +1050,7 @@ int dash_distill_grad(const float* logits, int64_t ld, int32_t rows, int32_t voc
 int dash_distill_loss_grad(const float* logits, int64_t ld, int32_t rows, int32_t vocab, const float* t_values,
                            const int32_t* t_indices, const float* t_rest, int32_t k, float temperature,
                            const float* d_weight, float* d_loss, void* d_grad, int64_t ld_grad, int32_t grad_dtype,
-                           void* stream) {
+                           void* ws, size_t ws_bytes, void* stream) {
     if (!logits || !t_values || !t_indices || !d_loss || !d_grad)
         return fail(DASH_EINVAL, "dash_distill_loss_grad: NULL argument");
     if (int rc = check_distill("dash_distill_loss_grad", ld, rows, vocab, k, temperature)) return rc;
@@ -1038,7 +1061,8 @@ int dash_distill_loss_grad(const float* logits, int64_t ld, int32_t rows, int32_
     a.grad = d_grad;
     a.ld_grad = ld_grad;
     a.grad_bf16 = grad_dtype == DASH_BF16;
-    DASH_HIP(launch_distill_grad(a, (hipStream_t)stream));
+    if (int rc = check_room("dash_distill_loss_grad", ws, ws_bytes, distill_workspace_bytes(rows, vocab))) return rc;
+    DASH_HIP(launch_distill_loss_grad(a, ws, (hipStream_t)stream));
     return DASH_OK;
 }
 

@@ -1,37 +1,33 @@
-// Selection of a row's K largest logits by one work-group (gfx950), shared by dash_top_logits and
-// the top-k draws of dash_sample_truncated.
+// Selection of a row's K largest logits (gfx950), shared by dash_top_logits and the top-k draws of
+// dash_sample_truncated.  Two launches.
 //
-// One pass: an entry above the bound `thr` (a value that K earlier entries reach) goes to a buffer
-// in LDS, every other one into the sum of the rest at once, so the rest needs no subtraction of
-// nearly equal sums.  After the first tile, then after doubling numbers of tiles, and whenever the
-// buffer could overflow, the buffer is cut back to about its K largest and thr rises to the least
-// of them.  Of random rows 1 + ln(V / 4096) times K entries then pass through the buffer; an
-// ascending row fills it every tile and is slower, never wrong.
+// The first walks the row (or stretches of it) once.  An entry above a bound that K entries reach goes
+// to a list in the workspace, every other one into the sum of the rest at once, so the rest needs no
+// subtraction of nearly equal sums.  The bound comes from four tiles spread over the row, which are
+// in registers before any is used: of each thread's largest of two tiles and largest of the other two,
+// the K-th.  About K / 16384 of a row is above it: 600 entries for K = 64.  This kernel does nothing else: with the
+// cuts below in it, its loop reloaded spilled addresses, and every such reload waits for all loads
+// in flight.
+//
+// The second gathers a row's lists in LDS, cuts them to the K largest and sorts those.  A list that
+// overflowed (a row that holds one value many times, or whose large values the sample misses) sends
+// it over the row itself, with a cut whenever the next tile might not fit.  That is slower, never wrong.
 //
 // Entries are held as one 64-bit word, key(l) : ~index, where key orders floats as unsigned
-// integers: a larger word is a larger logit, or an equal one at a lower index, and no two are
-// equal.  Cutting back bisects the words, seven pivots a step, counting with ballots.
+// integers: a larger word is a larger logit, or an equal one at a lower index, and no two are equal.
 #pragma once
+
+#include <algorithm>
 
 #include "row_walk.h"
 
 namespace dash {
 
 constexpr int kTopMax = 1024;             // largest K: one sorted entry per thread
-constexpr int kTopCap = 2 * kRowTile;     // buffer: what is kept and a whole tile, 64 KB of LDS
+constexpr int kTopCap = 2 * kRowTile;     // words in LDS: 64 KB, two work-groups per CU
 constexpr int kTopPer = kTopCap / kRowThreads;
+constexpr int kTopStart = 4;              // tiles that give the bound
 constexpr float kEvictOne = 17592186044416.f;  // 2^44: evicted terms are summed as integers of 2^-44
-
-struct TopShared {
-    uint64_t c[kTopCap];
-    uint64_t evict_z;
-    int added[3];      // entries appended in a tile, by turns
-    int piv[3][8];     // counts at or above the pivots, by turns
-    unsigned evict_ref;
-    int kept;
-    double red_d[kRowWaves];
-    float red_f[kRowWaves];
-};
 
 // Float order as unsigned order; -0 counts as +0 (equal values tie by index).
 DASH_DEV uint32_t top_key(float l) {
@@ -42,73 +38,107 @@ DASH_DEV float top_value(uint32_t key) { return __uint_as_float(key & 0x80000000
 DASH_DEV uint64_t top_word(float l, int i) { return (uint64_t)top_key(l) << 32 | (uint32_t)~i; }
 DASH_DEV float word_value(uint64_t w) { return top_value((uint32_t)(w >> 32)); }
 DASH_DEV int word_index(uint64_t w) { return (int)~(uint32_t)w; }
+// The largest float below the one with this key (that of no entry but -0's: +0 comes after the negative numbers).
+DASH_DEV float value_below(uint32_t key) { return top_value(key - (key == 0x80000000u ? 2u : 1u)); }
+constexpr uint32_t kKeyInf = 0xFF800000u;      // key(+inf): above every entry's
+constexpr uint32_t kKeyLowest = 0x00800000u;   // key of the lowest float
 
-// A row's selection: uniform over the work-group but for `rest`.
-struct TopState {
-    int n = 0;                // words in the buffer
-    int turn = 0;             // of `added`
-    int pturn = 0;            // of `piv`
-    float thr = -INFINITY;    // entries must exceed it
-    uint64_t low = 0;         // every word in the buffer is at or above it
-    ExpSum rest;              // the thread's share of the entries that were turned away
+// What the first launch leaves of a stretch: its rest, and the number of its words in the list (more
+// than the list's room: it overflowed).
+struct TopPart {
+    double z;  // sum of e^((l - ref) / T)
+    float ref;
+    int n;
+};
+// Stretches per row, and the room of a stretch's list: twice what the sampled bound lets
+// through on average.
+struct TopPlan {
+    RowSplit cut;
+    int room;
+};
+TopPlan top_plan(int rows, int vocab, int k);
+struct TopParts {
+    const TopPart* part;    // [rows][cut.n]
+    const uint64_t* words;  // [rows][cut.n][room]
+    int n, room;
+};
+hipError_t launch_top_parts(const float* logits, int64_t ld, int rows, int vocab, const int32_t* row_of, int k,
+                            float temperature, const TopPlan& plan, void* ws, TopParts& out, hipStream_t st);
+
+struct BoundShared {
+    int hist[kRowThreads];
+    int found[3];
+    int red_i[kRowWaves];
 };
 
-DASH_DEV void top_begin(TopShared& sh) {
-    if (threadIdx.x < 3) sh.added[threadIdx.x] = 0;
-    if (threadIdx.x < 24) (&sh.piv[0][0])[threadIdx.x] = 0;
-    __syncthreads();
-}
-
-// A word b with k <= (words at or above b) <= k + slack, where n >= k words are held as e.
-DASH_DEV uint64_t top_bound(TopShared& sh, TopState& st, const uint64_t (&e)[kTopPer], int k, int slack, int& count) {
-    uint64_t lo = st.low, hi = 0xFF80000000000000ull;  // key(+inf): no word reaches it
-    count = st.n;
+// A bound b with k <= (words e at or above b), and at most k + slack unless equal words straddle that;
+// lo <= b < hi, count words are at or above lo, none at or above hi.  The first `per` of a thread's
+// words count.  A histogram of the range in 1024 parts, summed from the top, finds the part that holds
+// the k-th word; that part is the range of the next round, if it holds too many.  Two rounds as a rule.
+template <class W, int PER>
+DASH_DEV W top_bound(BoundShared& sh, const W (&e)[PER], int per, int k, int slack, W lo, W hi, int& count) {
+    int above = 0;  // words at or above hi
     while (count > k + slack && hi - lo > 1) {
-        const uint64_t step = max((hi - lo) >> 3, (uint64_t)1);
-        int c[8] = {};
-#pragma unroll
-        for (int r = 0; r < kTopPer; ++r) {
-            if (r * kRowThreads >= st.n) break;
-#pragma unroll
-            for (int j = 1; j < 8; ++j) c[j] += __popcll(__ballot(e[r] >= lo + j * step));
-        }
-        int* cnt = sh.piv[st.pturn];
-        if ((threadIdx.x & 63) == 0) {
-#pragma unroll
-            for (int j = 1; j < 8; ++j)
-                if (c[j]) atomicAdd(&cnt[j], c[j]);
-        }
-        st.pturn = st.pturn == 2 ? 0 : st.pturn + 1;
+        const int bits = (int)(8 * sizeof(uint64_t)) - __clzll((unsigned long long)(hi - lo - 1));
+        const int shift = max(bits - 10, 0);
         __syncthreads();
-        // Cleared for the step after next: every thread has read it before this barrier, and adds to
-        // it only after the next one.
-        if (threadIdx.x < 8) sh.piv[st.pturn == 2 ? 0 : st.pturn + 1][threadIdx.x] = 0;
-        uint64_t next_lo = lo, next_hi = lo + step;
+        sh.hist[threadIdx.x] = 0;
+        __syncthreads();
 #pragma unroll
-        for (int j = 1; j < 8; ++j) {
-            const int at = cnt[j];
-            if (at >= k) {
-                next_lo = lo + j * step;
-                next_hi = j < 7 ? next_lo + step : hi;
-                count = at;
-            }
+        for (int r = 0; r < PER; ++r) {
+            if (r >= per) break;
+            if (e[r] >= lo && e[r] < hi) atomicAdd(&sh.hist[(int)((e[r] - lo) >> shift)], 1);
         }
-        lo = next_lo;
-        hi = min(hi, next_hi);
+        __syncthreads();
+        const int part = kRowThreads - 1 - (int)threadIdx.x, here = sh.hist[part];
+        int total;
+        const int upto = above + block_scan(here, sh.red_i, total);
+        if (upto >= k && upto - here < k) {
+            sh.found[0] = part;
+            sh.found[1] = upto;
+            sh.found[2] = upto - here;
+        }
+        __syncthreads();
+        lo += (W)sh.found[0] << shift;
+        const W top = lo + ((W)1 << shift);
+        hi = top < hi && top > lo ? top : hi;
+        count = sh.found[1];
+        above = sh.found[2];
     }
     return lo;
 }
 
-// Cuts the buffer back to k .. k + slack words (n > k + slack); what falls out joins the rest.
+// ---- the second launch: a row's words in LDS ---------------------------------------------------
+
+struct TopShared {
+    uint64_t c[kTopCap];
+    uint64_t evict_z;
+    int count;         // words appended
+    unsigned evict_ref;
+    int kept;
+    BoundShared bound;
+    double red_d[kRowWaves];
+    float red_f[kRowWaves];
+};
+// Uniform over the work-group but for `rest`.
+struct TopState {
+    int n = 0;       // words in the buffer, as of the last barrier that counted
+    uint64_t low = 0;  // words must reach this
+    ExpSum rest;     // the thread's share of the entries that were turned away
+};
+
+// Cuts the buffer from n > k + slack words to k .. k + slack; what falls out joins the rest, and the
+// bound rises to the least word left.  Between barriers that separate it from appends.
 DASH_DEV void top_cut(TopShared& sh, TopState& st, int k, int slack, float scale) {
+    const int per = (st.n + kRowThreads - 1) / kRowThreads;
     uint64_t e[kTopPer];
 #pragma unroll
     for (int r = 0; r < kTopPer; ++r) {
         const int i = r * kRowThreads + (int)threadIdx.x;
         e[r] = i < st.n ? sh.c[i] : 0;
     }
-    int count;
-    const uint64_t b = top_bound(sh, st, e, k, slack, count);
+    int count = st.n;
+    const uint64_t b = top_bound(sh.bound, e, per, k, slack, (uint64_t)kKeyLowest << 32, (uint64_t)kKeyInf << 32, count);
     if (threadIdx.x == 0) {
         sh.evict_z = 0;
         sh.evict_ref = 0;
@@ -118,7 +148,7 @@ DASH_DEV void top_cut(TopShared& sh, TopState& st, int k, int slack, float scale
     unsigned out = 0;  // the largest key that falls out
 #pragma unroll
     for (int r = 0; r < kTopPer; ++r) {
-        if (r * kRowThreads >= st.n) break;
+        if (r >= per) break;
         const uint64_t keep = __ballot(e[r] >= b);
         if (keep) {
             int at = 0;
@@ -138,7 +168,7 @@ DASH_DEV void top_cut(TopShared& sh, TopState& st, int k, int slack, float scale
         uint64_t z = 0;
 #pragma unroll
         for (int r = 0; r < kTopPer; ++r) {
-            if (r * kRowThreads >= st.n) break;
+            if (r >= per) break;
             if (e[r] && e[r] < b) z += (uint64_t)(__builtin_amdgcn_exp2f((word_value(e[r]) - ref) * scale) * kEvictOne);
         }
         if (z) atomicAdd((unsigned long long*)&sh.evict_z, (unsigned long long)z);
@@ -153,92 +183,121 @@ DASH_DEV void top_cut(TopShared& sh, TopState& st, int k, int slack, float scale
             }
         }
     }
+    if (threadIdx.x == 0) sh.count = count;
     st.n = count;
     st.low = b;
-    st.thr = word_value(b);
+    __syncthreads();
 }
 
-// One tile of the row (tile number t) into the selection.
-DASH_DEV void top_tile(TopShared& sh, TopState& st, f32x4_t l, int i, int k, float scale) {
-#pragma unroll
-    for (int j = 0; j < 4; ++j) l[j] = fmaxf(l[j], -INFINITY);  // NaN is no entry
-    float m4 = max4(l);
-    if (__any(m4 > st.thr)) {
-        uint64_t in[4];
-        int total = 0;
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            in[j] = __ballot(l[j] > st.thr && l[j] < INFINITY);
-            total += __popcll(in[j]);
+// Appends the words of those lanes that have one (any lanes of a wave).
+DASH_DEV void top_append(TopShared& sh, bool mine, uint64_t word) {
+    const uint64_t in = __ballot(mine);
+    if (!in) return;
+    int at = 0;
+    if ((threadIdx.x & 63) == 0) at = atomicAdd(&sh.count, __popcll(in));
+    at = __builtin_amdgcn_readfirstlane(at);
+    if (mine) sh.c[at + __popcll(in & ((1ull << (threadIdx.x & 63)) - 1))] = word;
+}
+// After at most kRowTile appends: room for as many again.
+DASH_DEV void top_count(TopShared& sh, TopState& st, int k, float scale) {
+    __syncthreads();
+    st.n = sh.count;
+    __syncthreads();
+    if (st.n > kTopCap - kRowTile) top_cut(sh, st, k, (k >> 2) + 32, scale);
+}
+
+// The words of row b among them the k largest, and the rest of the row.
+DASH_DEV void top_gather(TopShared& sh, TopState& st, const TopParts& p, int64_t b, const float* row, int vocab, int k,
+                         float scale) {
+    if (threadIdx.x == 0) sh.count = 0;
+    const TopPart* part = p.part + b * p.n;
+    const uint64_t* words = p.words + b * p.n * p.room;
+    bool fits = true;
+    if ((int)threadIdx.x < p.n) {
+        const TopPart mine = part[threadIdx.x];
+        fits = mine.n <= p.room;
+        if (mine.z > 0.0) {
+            st.rest.ref = mine.ref;
+            st.rest.z = mine.z;
         }
-        int at = 0;
-        if ((threadIdx.x & 63) == 0 && total) at = atomicAdd(&sh.added[st.turn], total);
-        at = __builtin_amdgcn_readfirstlane(at) + st.n;
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const bool mine = l[j] > st.thr;
-            if (mine && l[j] < INFINITY)
-                sh.c[at + __popcll(in[j] & ((1ull << (threadIdx.x & 63)) - 1))] = top_word(l[j], i + j);
-            if (mine) l[j] = -INFINITY;  // +inf is no entry either
-            at += __popcll(in[j]);
-        }
-        m4 = max4(l);
     }
-    exp_push4<false>(st.rest, l, m4, scale);
-    __syncthreads();
-    st.n += sh.added[st.turn];
-    // Cleared for the tile after next (as the pivots' counts).
-    if (threadIdx.x == 0) sh.added[st.turn == 0 ? 2 : st.turn - 1] = 0;
-    st.turn = st.turn == 2 ? 0 : st.turn + 1;
-}
-
-// Entries [lo, hi) of the row into the buffer, which ends with at most max(kTopCap - kRowTile, ...)
-// words; thr and the rest as described above.
-DASH_DEV void top_walk(TopShared& sh, TopState& st, const float* row, int lo, int hi, int k, float scale) {
-    int tile = 0, next = 1;
-    const int slack = (k >> 2) + 32;
-    walk_row<4, true>(row, lo, hi, [&](const f32x4_t& l, int i) {
-        top_tile(sh, st, l, i, k, scale);
-        ++tile;
-        if (st.n > kTopCap - kRowTile || (tile >= next && st.n > k + slack)) {
-            top_cut(sh, st, k, slack, scale);
-            next = 2 * tile;
-        }
-    });
-}
-
-// Leaves the m = min(n, k) largest words sorted in sh.c[0 .. m), descending; returns m.
-DASH_DEV int top_finish(TopShared& sh, TopState& st, int k, float scale) {
-    __syncthreads();
-    if (st.n > k) top_cut(sh, st, k, 0, scale);
-    const int m = st.n;
-    int p = 2;
-    while (p < m) p <<= 1;
-    __syncthreads();
-    for (int i = m + (int)threadIdx.x; i < p; i += kRowThreads) sh.c[i] = 0;
-    __syncthreads();
-    for (int size = 2; size <= p; size <<= 1) {
-        for (int d = size >> 1; d >= 1; d >>= 1) {
-            if ((int)threadIdx.x < p >> 1) {
-                const int a = (((int)threadIdx.x & ~(d - 1)) << 1) | ((int)threadIdx.x & (d - 1));
-                const uint64_t x = sh.c[a], y = sh.c[a + d];
-                const bool down = (a & size) == 0;
-                if (down ? x < y : x > y) {
-                    sh.c[a] = y;
-                    sh.c[a + d] = x;
-                }
+    if (__syncthreads_and(fits)) {
+        for (int from = 0; from < p.n * p.room; from += kRowTile) {  // (room is a multiple of 64: a wave has one list)
+#pragma unroll
+            for (int r = 0; r < kRowTile / kRowThreads; ++r) {
+                const int i = from + r * kRowThreads + (int)threadIdx.x;
+                if (i >= p.n * p.room) break;
+                const bool in = i % p.room < part[i / p.room].n;
+                top_append(sh, in, in ? words[i] : 0);
             }
-            __syncthreads();
+            top_count(sh, st, k, scale);
         }
+        return;
+    }
+    st = TopState{};
+    for (int at = 0; at < vocab; at += kRowTile) {
+        walk_row<1, true>(row, at, min(vocab, at + kRowTile), [&](f32x4_t l, int i) {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const bool entry = fabsf(l[j]) < INFINITY;
+                const uint64_t w = entry ? top_word(l[j], i + j) : 0;
+                const bool in = entry && w >= st.low;
+                top_append(sh, in, w);
+                if (in || !entry) l[j] = -INFINITY;
+            }
+            exp_push4<false>(st.rest, l, max4(l), scale);
+        });
+        top_count(sh, st, k, scale);
+    }
+}
+
+// Leaves the m = min(n, k) largest words sorted in sh.c[0 .. m), descending (what lies behind them in
+// the buffer is added to the rest); returns m.
+DASH_DEV int top_finish(TopShared& sh, TopState& st, int k, float scale) {
+    int p = 64;
+    while (p < k) p <<= 1;
+    __syncthreads();
+    if (st.n > p) top_cut(sh, st, k, p - k, scale);
+    const int n = st.n;
+    for (int i = n + (int)threadIdx.x; i < p; i += kRowThreads) sh.c[i] = 0;
+    __syncthreads();
+    if (p <= 128) {
+        // A word's place is the number of larger ones (words differ; zeros fill what is left):
+        // kRowThreads / p threads per word count over a share of the words each.
+        const int i = (int)threadIdx.x & (p - 1), share = (int)threadIdx.x / p, len = p * p / kRowThreads;
+        const uint64_t mine = sh.c[i];
+        int place = 0;
+        for (int j = share * len; j < (share + 1) * len; ++j) place += sh.c[j] > mine;
+        sh.bound.hist[threadIdx.x] = place;
+        __syncthreads();
+        if ((int)threadIdx.x < p) {
+            for (int q = 1; q < kRowThreads / p; ++q) place += sh.bound.hist[threadIdx.x + q * p];
+            if (mine) sh.c[place] = mine;  // (each thread has its own word in a register)
+        }
+    } else {
+        for (int size = 2; size <= p; size <<= 1) {
+            for (int d = size >> 1; d >= 1; d >>= 1) {
+                if ((int)threadIdx.x < p >> 1) {
+                    const int a = (((int)threadIdx.x & ~(d - 1)) << 1) | ((int)threadIdx.x & (d - 1));
+                    const uint64_t x = sh.c[a], y = sh.c[a + d];
+                    const bool down = (a & size) == 0;
+                    if (down ? x < y : x > y) {
+                        sh.c[a] = y;
+                        sh.c[a + d] = x;
+                    }
+                }
+                __syncthreads();
+            }
+        }
+    }
+    __syncthreads();
+    const int m = min(n, k);
+    const int i = m + (int)threadIdx.x;
+    if (__any(i < n)) {
+        const float l = i < n ? word_value(sh.c[i]) : -INFINITY;
+        exp_push4<false>(st.rest, f32x4_t{l, -INFINITY, -INFINITY, -INFINITY}, l, scale);
     }
     return m;
-}
-
-// Sum of the rest over the work-group: e^((x - ref) / T) summed, and ref (0 and -FLT_MAX: nothing).
-DASH_DEV double top_rest(TopShared& sh, const TopState& st, double temperature, float& ref) {
-    ref = block_max_f(st.rest.z > 0.0 ? st.rest.ref : -FLT_MAX, sh.red_f);
-    const double z = st.rest.z > 0.0 ? st.rest.z * exp(((double)st.rest.ref - (double)ref) / temperature) : 0.0;
-    return block_sum_d(z, sh.red_d);
 }
 
 }  // namespace dash

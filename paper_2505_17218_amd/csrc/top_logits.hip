@@ -7,14 +7,82 @@ namespace dash {
 
 namespace {
 
+constexpr int kTopTarget = 512, kTopStretch = 4096, kTopParts = 64, kTopRoom = 16384;
+
+__global__ void __launch_bounds__(kRowThreads, 8)
+top_part_k(const float* __restrict__ logits, int64_t ld, int vocab, const int32_t* __restrict__ row_of, int k,
+           double temperature, float scale, TopPlan plan, TopPart* __restrict__ part, uint64_t* __restrict__ words) {
+    __shared__ BoundShared bound;
+    __shared__ int count;
+    __shared__ double red_d[kRowWaves];
+    __shared__ float red_f[kRowWaves];
+    const int64_t b = blockIdx.x / plan.cut.n;
+    const int lo = (int)(blockIdx.x % plan.cut.n) * plan.cut.len;
+    const float* row = logits + (row_of ? (int64_t)row_of[b] : b) * ld;
+    words += (int64_t)blockIdx.x * plan.room;
+    if (threadIdx.x == 0) count = 0;
+    __syncthreads();
+    float thr = -INFINITY;  // entries in the list exceed it
+    ExpSum rest;
+    walk_row<kTopStart, true, true>(
+        row, lo, min(vocab, lo + plan.cut.len),
+        [&](const f32x4_t (&buf)[kTopStart], int whole) {
+            uint32_t e[kTopStart / 2];
+            const int real = min(max(whole, 1), kTopStart);  // the places behind repeat a tile
+#pragma unroll
+            for (int h = 0; h < kTopStart / 2; ++h) {
+                float m = -INFINITY;
+#pragma unroll
+                for (int d = 2 * h; d < 2 * h + 2; ++d)
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) m = fmaxf(m, d < real && buf[d][j] < INFINITY ? buf[d][j] : -INFINITY);
+                e[h] = m > -INFINITY ? top_key(m) : 0u;
+            }
+            int n = kTopStart / 2 * kRowThreads;
+            // (no bound where the sample holds fewer than k entries)
+            const uint32_t low = top_bound(bound, e, kTopStart / 2, k, k >> 3, 0u, kKeyInf, n);
+            if (low >= kKeyLowest) thr = value_below(low);
+            thr = __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(thr)));
+        },
+        [&](f32x4_t l, int i) {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) l[j] = fmaxf(l[j], -INFINITY);  // NaN is no entry
+            if (__any(max4(l) > thr)) {
+                uint64_t in[4];
+                int total = 0;
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    in[j] = __ballot(l[j] > thr && l[j] < INFINITY);
+                    total += __popcll(in[j]);
+                }
+                int at = 0;
+                if ((threadIdx.x & 63) == 0) at = atomicAdd(&count, total);
+                at = __builtin_amdgcn_readfirstlane(at);
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const int to = at + (int)__builtin_amdgcn_mbcnt_hi((uint32_t)(in[j] >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)in[j], 0u));
+                    if (l[j] > thr) {
+                        if (l[j] < INFINITY && to < plan.room) words[to] = top_word(l[j], i + j);
+                        l[j] = -INFINITY;  // (+inf is no entry either)
+                    }
+                    at += __popcll(in[j]);
+                }
+            }
+            exp_push4<false>(rest, l, max4(l), scale);
+        },
+        [](int) { return false; });
+    float ref;
+    const double z = block_exp_sum(rest, temperature, red_f, red_d, ref);
+    if (threadIdx.x == 0) part[blockIdx.x] = TopPart{z, ref, count};
+}
+
 __global__ void __launch_bounds__(kRowThreads)
 top_logits_k(const float* __restrict__ logits, int64_t ld, int vocab, int k, double temperature, float scale,
-             float* __restrict__ values, int32_t* __restrict__ indices, float* __restrict__ rest) {
+             TopParts parts, float* __restrict__ values, int32_t* __restrict__ indices, float* __restrict__ rest) {
     __shared__ TopShared sh;
     const int64_t r = blockIdx.x;
     TopState st;
-    top_begin(sh);
-    top_walk(sh, st, logits + r * ld, 0, vocab, k, scale);
+    top_gather(sh, st, parts, r, logits + r * ld, vocab, k, scale);
     const int m = top_finish(sh, st, k, scale);
     if ((int)threadIdx.x < k) {
         const bool some = (int)threadIdx.x < m;
@@ -24,7 +92,7 @@ top_logits_k(const float* __restrict__ logits, int64_t ld, int vocab, int k, dou
     }
     if (!rest) return;
     float ref;
-    const double z = top_rest(sh, st, temperature, ref);
+    const double z = block_exp_sum(st.rest, temperature, sh.red_f, sh.red_d, ref);
     if (threadIdx.x == 0) rest[r] = z > 0.0 ? (float)((double)ref / temperature + log(z)) : -INFINITY;
 }
 
@@ -32,10 +100,40 @@ top_logits_k(const float* __restrict__ logits, int64_t ld, int vocab, int k, dou
 
 int top_logits_max() { return kTopMax; }
 
+TopPlan top_plan(int rows, int vocab, int k) {
+    auto room = [&](int len) {  // words let through: about k in every kTopStart tiles
+        const int64_t want = 2 * (int64_t)k * std::max(len / (kTopStart * kRowTile), 1) + 64;
+        int r = 256;
+        while (r < want && r < kTopRoom) r <<= 1;
+        return r;
+    };
+    TopPlan p;
+    p.cut = split_row(vocab, std::min({kTopParts, kTopTarget / std::max(rows, 1), vocab / kTopStretch}));
+    p.room = room(p.cut.len);
+    return p;
+}
+size_t top_workspace_bytes(int rows, int vocab, int k) {
+    const TopPlan p = top_plan(rows, vocab, k);
+    return (size_t)rows * p.cut.n * (sizeof(TopPart) + sizeof(uint64_t) * p.room);
+}
+
+hipError_t launch_top_parts(const float* logits, int64_t ld, int rows, int vocab, const int32_t* row_of, int k,
+                            float temperature, const TopPlan& plan, void* ws, TopParts& out, hipStream_t st) {
+    TopPart* part = (TopPart*)ws;
+    uint64_t* words = (uint64_t*)(part + (size_t)rows * plan.cut.n);
+    out = TopParts{part, words, plan.cut.n, plan.room};
+    top_part_k<<<rows * plan.cut.n, kRowThreads, 0, st>>>(logits, ld, vocab, row_of, k, (double)temperature,
+                                                          exp2_scale(temperature), plan, part, words);
+    return hipGetLastError();
+}
+
 hipError_t launch_top_logits(const float* logits, int64_t ld, int rows, int vocab, int k, float temperature,
-                             float* values, int32_t* indices, float* rest, hipStream_t st) {
+                             float* values, int32_t* indices, float* rest, void* ws, hipStream_t st) {
     if (rows <= 0) return hipSuccess;
-    top_logits_k<<<rows, kRowThreads, 0, st>>>(logits, ld, vocab, k, (double)temperature, exp2_scale(temperature),
+    TopParts p;
+    if (hipError_t e = launch_top_parts(logits, ld, rows, vocab, nullptr, k, temperature, top_plan(rows, vocab, k), ws, p, st))
+        return e;
+    top_logits_k<<<rows, kRowThreads, 0, st>>>(logits, ld, vocab, k, (double)temperature, exp2_scale(temperature), p,
                                                values, indices, rest);
     return hipGetLastError();
 }

@@ -12,11 +12,22 @@
 // No top-k: nothing is sorted.  The draw over a set that contains the kept tokens, if it is itself
 // kept, is the draw over the kept tokens (the largest score of a superset); if not, no kept token
 // comes after it in the order, and the draw is repeated over the tokens before it, a smaller set that
-// still contains every kept one.  So a row costs one pass of noise, as dash_sample, then one
-// pass that sums the mass before the winner, and a row's winner is kept with probability
-// top_p; 1 + ln(1 / top_p) draws are expected from a flat row.  The mass is compared in float32
-// exponentials first; only where it is within kMassTol of the border, the sums are repeated in
-// float64, so the decision is that of float64 sums.
+// still contains every kept one.
+//   draw_first   the draw over the row, its exponential sum, and (top_p) a histogram of its mass over the
+//                logit, 32 parts per power of two.  The histogram tells from the winner's logit
+//                whether it is kept, unless it lies within two parts of the border: at
+//                top_p = 0.95 about 95 rows in 100 end here.  With min-p the draw leaves out at once
+//                what is too far below the largest logit so far.
+//   draw_second  rows that did not end: the mass before the winner, and at once the draw over the
+//                tokens before it that the histogram does not rule out; each row cut into stretches,
+//                so that few rows still fill the GPU.
+//   draw_last    joins these; the second winner is nearly always settled by the histogram, too.  What is
+//                left takes further passes of one work-group.
+// Few rows are cut into stretches in the first pass as well, joined by draw_join.
+// Masses are float32 exponentials first; only where they are within kMassTol of the border, the sums
+// are repeated in float64, so the decision is that of float64 sums.
+#include <type_traits>
+
 #include "kernels.h"
 #include "sampler_screen.h"
 #include "top_logits.h"
@@ -30,6 +41,9 @@ namespace {
 // scale, product) and the exponential's 2^-23; averaged over a row's mass y is at most log2(vocab)
 // <= 28.  Together below 4e-6 for either sum; sums in float64 add nothing.
 constexpr double kMassTol = 1e-5;
+
+constexpr int kDrawTarget = 512;   // work-groups that fill the GPU
+constexpr int kDrawStretch = 4096;  // least entries of a stretch
 
 struct Draw {
     const float* logits;
@@ -59,12 +73,13 @@ DASH_DEV float noise_of(const Draw& a, int i, uint32_t step, uint32_t uid) {
     return gumbel_from_bits(i & 2 ? hi : lo);
 }
 
-// Largest score of the work-group, smallest index on ties (INT_MAX: none); every thread gets it.
+// Largest score of the work-group, smallest index on ties (kNone: none); every thread gets both.
+constexpr int kNone = 0x7FFFFFFF;
 struct BestShared {
     float s[kRowWaves];
     int i[kRowWaves];
 };
-DASH_DEV int block_best(float s, int i, BestShared& sh) {
+DASH_DEV void block_best(float& s, int& i, BestShared& sh) {
 #pragma unroll
     for (int o = 32; o >= 1; o >>= 1) {
         const float os = __shfl_xor(s, o, 64);
@@ -88,57 +103,38 @@ DASH_DEV int block_best(float s, int i, BestShared& sh) {
             s = sh.s[w];
             i = sh.i[w];
         }
-    return i;
-}
-
-// Inclusive sum of v over the threads up to this one, and the total, in float64.
-DASH_DEV double block_scan(double v, double* red, double& total) {
-    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) {
-        const double u = __shfl_up(v, o, 64);
-        if (lane >= o) v += u;
-    }
-    __syncthreads();
-    if (lane == 63) red[w] = v;
-    __syncthreads();
-    double before = 0.0;
-    total = 0.0;
-    for (int i = 0; i < kRowWaves; ++i) {
-        if (i < w) before += red[i];
-        total += red[i];
-    }
-    return v + before;
 }
 
 template <bool UNIT_T>
 __global__ void __launch_bounds__(kRowThreads)
-draw_top_k(Draw a) {
+draw_top_k(Draw a, TopParts parts) {
     __shared__ TopShared sh;
     __shared__ BestShared best;
     const int b = blockIdx.x;
     const float* row = a.logits + (int64_t)(a.row_of ? a.row_of[b] : b) * a.ld;
     TopState st;
-    top_begin(sh);
-    top_walk(sh, st, row, 0, a.vocab, a.top_k, a.scale);
+    top_gather(sh, st, parts, b, row, a.vocab, a.top_k, a.scale);
     const int m = top_finish(sh, st, a.top_k, a.scale);
     const double T = a.temperature;
     float ref;
-    const double rest = top_rest(sh, st, T, ref);
+    const double rest = block_exp_sum(st.rest, T, sh.red_f, sh.red_d, ref);
     const bool in = (int)threadIdx.x < m;
     const uint64_t word = in ? sh.c[threadIdx.x] : 0;
     const float l = word_value(word), l0 = word_value(sh.c[0]);
-    const int i = word_index(word);
     const double w = in ? exp(((double)l - (double)l0) / T) : 0.0;
     double total;
     const double upto = block_scan(w, sh.red_d, total);
     bool keep = in && (a.top_p >= 1.0 || upto - w < a.top_p * total);
     keep = keep && (double)l >= (double)l0 + T * a.log_min_p;
     float s = -INFINITY;
-    if (keep) s = (UNIT_T ? l : div_rn(l, a.temperature)) + noise_of(a, i, (uint32_t)a.step[b], (uint32_t)a.uid[b]);
-    const int tok = block_best(s, keep ? i : 0x7FFFFFFF, best);
+    int tok = kNone;
+    if (keep) {
+        tok = word_index(word);
+        s = (UNIT_T ? l : div_rn(l, a.temperature)) + noise_of(a, tok, (uint32_t)a.step[b], (uint32_t)a.uid[b]);
+    }
+    block_best(s, tok, best);
     if (threadIdx.x != 0) return;
-    if (tok == 0x7FFFFFFF) {
+    if (tok == kNone) {
         write_draw(a, b, -1, 0.0);
     } else {
         const double all = total + (rest > 0.0 ? rest * exp(((double)ref - (double)l0) / T) : 0.0);
@@ -146,58 +142,147 @@ draw_top_k(Draw a) {
     }
 }
 
-// What a pass of noise may draw from: entries before (l, i) in the order, at or above `low`.
-struct Before {
-    float l;
-    int i;
-    float low;
+// ---- without top-k ----------------------------------------------------------------------------
+
+// ---- without top-k ----------------------------------------------------------------------------
+
+// Histogram of a row's mass: an exponential e relative to a reference logit falls into the part that
+// its exponent and the five bits below it name; there are 1024, one per thread, from 20 octaves
+// below the reference to 12 above (an entry further above voids the histogram).  A part is summed in integers, the leading 14 bits of each e, so
+// sums do not depend on order: 2^18 terms fit, and what is cut off is less than 2^-13 of each.
+// (Float atomics in LDS took five times as long as everything else.)  Lanes add to four copies.
+constexpr int kBins = kRowThreads;
+constexpr int kBinsPerOctave = 32;
+constexpr int kBinsBelow = 20, kBinsAbove = kBins / kBinsPerOctave - kBinsBelow;  // octaves
+constexpr uint32_t kBinBase = (127 - kBinsBelow) * kBinsPerOctave;
+constexpr int kCopies = 4;
+constexpr int kHistVocab = 1 << 18;
+constexpr double kBinTol = 1.3e-4;  // 2^-13, rounded up
+DASH_DEV int bin_of(float e) { return min(max((int)(__float_as_uint(e) >> 18) - (int)kBinBase, 0), kBins - 1); }
+DASH_DEV uint32_t bin_term(float e) { return __builtin_amdgcn_ubfe(__float_as_uint(e), 10, 13) | 0x2000u; }
+// Value of a sum of terms of bin i.  (Entries below the lowest bin join it and count for more than they
+// are; that moves only the mass at or above bin 0, which rules nothing out and settles nothing.)
+DASH_DEV double bin_mass(uint32_t sum, int i) { return ldexp((double)sum, i / kBinsPerOctave - kBinsBelow - 13); }
+
+// What a work-group that walked a stretch of a row in draw_first leaves.
+struct FirstPart {
+    double z;         // sum of e^((l - ref) / T)
+    float ref, top;   // top: largest logit
+    float bins_at;    // reference of the bins, octaves: a whole number; NaN: no histogram
+    float s;          // largest score and its token
+    int i, pad;
 };
-DASH_DEV bool comes_before(float l, int i, const Before& w) {
-    return (l > w.l || (l == w.l && i < w.i)) && l < INFINITY && l >= w.low;
+// A row that has not ended: its winner, and what it takes to settle it.
+struct RowState {
+    double z;         // sum of e^((l - top) / T)
+    float l, top, low;  // the winner's logit, the largest, the least that min-p keeps
+    float bin_ref;    // reference logit of the bins; NaN: no histogram
+    int tok;
+    int unsure;       // the winner may be kept
+    int border, sure; // tokens of bins below border are not kept, of bins from sure on they are
+};
+struct SecondPart {
+    double before;  // sum of e^((l - top) / T) before the winner
+    float s;        // draw over the tokens before it
+    int i;
+};
+
+// The logit that lies n octaves from zero.
+DASH_DEV float octaves(float n, float temperature) { return (float)((double)n * 0.6931471805599453 * (double)temperature); }
+
+DASH_DEV bool kept_by_own_mass(const Draw& a, float l, float top, double z) {
+    // all but the winner's own mass is at least what comes before it
+    return 1.0 - exp(((double)l - (double)top) / (double)a.temperature) / z < a.top_p - kMassTol;
 }
 
-// The draw over a row's entries (ALL: every finite one; else those that come before w), screened as
-// in sampler.hip.  ALL also sums the row's exponentials and finds its largest logit.
-template <bool UNIT_T, bool ALL>
-DASH_DEV int draw_row(const Draw& a, const float* row, uint32_t step, uint32_t uid, const Before& w, float* floor_s,
-                      BestShared& best, ExpSum& sum, float& top) {
-    float best_s = -INFINITY;
-    int best_i = 0x7FFFFFFF;
-    const float inv_t = UNIT_T ? 1.f : div_rn(1.f, a.temperature);
-    __syncthreads();
-    if (threadIdx.x == 0) *floor_s = -INFINITY;
-    __syncthreads();
-    walk_row<2, false>(row, 0, a.vocab, [&](f32x4_t l, int i) {
-        bool some = false;
+// Settles a row after its first draw, or leaves its state.  bin: the mass of this thread's bin.
+struct SettleShared {
+    double red[kRowWaves];
+    int red_i[kRowWaves];
+};
+DASH_DEV void settle(const Draw& a, int b, const float* row, int tok, float top, double z, float bin_ref, double bin,
+                     SettleShared& sh, RowState* state, int* open) {
+    bool done = true;
+    RowState r{z, 0.f, top, -INFINITY, bin_ref, tok, 0, -kBins, 2 * kBins};
+    if (tok != kNone) {
+        const double T = a.temperature;
+        r.l = row[tok];
+        // the least float at or above the min-p border
+        const double t = (double)top + T * a.log_min_p;
+        r.low = (float)t;
+        if ((double)r.low < t) r.low = nextafterf(r.low, INFINITY);
+        const bool reaches = r.l >= r.low;
+        done = reaches && (a.top_p >= 1.0 || kept_by_own_mass(a, r.l, top, z));
+        if (!done && a.top_p < 1.0) {
+            r.unsure = reaches;
+            if (bin_ref == bin_ref) {
+                // Mass at or above each bin, with one bin either way for logits that other stretches or
+                // the exponential's last bit put into a neighbouring bin.
+                double all;
+                const double below = block_scan(bin, sh.red, all);
+                const double from = all - below + bin, tol = (kMassTol + kBinTol) * z;
+                auto most = [](int x, int y) { return max(x, y); };
+                const int last = block_reduce(from >= a.top_p * z - tol ? (int)threadIdx.x : -kBins, sh.red_i, most);
+                const int whole = block_reduce(from >= a.top_p * z + tol ? (int)threadIdx.x : -kBins, sh.red_i, most);
+                r.sure = last + 2;
+                r.border = whole - 1;
+                const int at = bin_of(__builtin_amdgcn_exp2f((r.l - bin_ref) * a.scale));
+                done = reaches && at >= r.sure;
+                r.unsure = reaches && at >= r.border;
+            }
+        }
+    }
+    if (threadIdx.x != 0) return;
+    open[b] = !done;
+    if (!done) state[b] = r;
+    else if (tok == kNone) write_draw(a, b, -1, 0.0);
+    else write_draw(a, b, tok, ((double)r.l - (double)top) / (double)a.temperature - log(z));
+}
+
+// Replaces what is no entry by -inf.  A finite sum of the four shows that all are.
+DASH_DEV void finite_or_low(f32x4_t& l) {
+    if (__any(!(fabsf((l[0] + l[1]) + (l[2] + l[3])) < INFINITY))) {
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const bool in = ALL ? fabsf(l[j]) < INFINITY : comes_before(l[j], i + j, w);
-            l[j] = in ? l[j] : -INFINITY;
-            some |= in;
-        }
-        if (!__any(some)) return;
-        const float m4 = max4(l);
-        if constexpr (ALL) {
-            top = fmaxf(top, m4);
-            exp_push4<false>(sum, l, m4, a.scale);
-        }
+        for (int j = 0; j < 4; ++j) l[j] = fabsf(l[j]) < INFINITY ? l[j] : -INFINITY;
+    }
+}
+
+// The draw over a stretch of a row, screened as in sampler.hip: thread and work-group state.
+template <bool UNIT_T>
+struct Drawing {
+    float s = -INFINITY;
+    int i = kNone;
+    uint32_t step, uid;
+    float inv_t;
+    float* floor_s;  // lower bound on the best exact score that the work-group has seen
+
+    // Clears the shared bound; the caller's next barrier is before the first score4.
+    DASH_DEV Drawing(const Draw& a, int b, float* floor) : floor_s(floor) {
+        step = (uint32_t)a.step[b];
+        uid = (uint32_t)a.uid[b];
+        inv_t = UNIT_T ? 1.f : div_rn(1.f, a.temperature);
+        if (threadIdx.x == 0) *floor_s = -INFINITY;
+    }
+    // Entries i0 .. i0+3; those that are -inf take no part.
+    DASH_DEV void score4(const Draw& a, const f32x4_t& l, int i0) {
         // Relaxed: a stale bound is a lower one, and only more entries are evaluated.
         const float floor_w = __hip_atomic_load(floor_s, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
-        const U4 x = philox4x32_10(U4{(uint32_t)i >> 2, step, uid, 0u}, a.k0, a.k1);
+        uint32_t k0 = a.k0, k1 = a.k1;
+        asm volatile("" : "+s"(k0), "+s"(k1));  // the round keys are derived here, not kept
+        const U4 x = philox4x32_10(U4{(uint32_t)i0 >> 2, step, uid, 0u}, k0, k1);
         float sc[4];
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
             // l / T by a product and one corrected step, within the margin of the exact quotient, or
-            // NaN where something overflows (then nothing is screened)
+            // NaN where something overflows (then nothing is screened; so too for an entry of -inf)
             const float q = l[j] * inv_t;
             sc[j] = UNIT_T ? l[j] : __builtin_fmaf(__builtin_fmaf(-q, a.temperature, l[j]), inv_t, q);
-            if (l[j] == -INFINITY) sc[j] = -INFINITY;
         }
         float hi4 = sc[0];
 #pragma unroll
         for (int j = 1; j < 4; ++j) hi4 = UNIT_T ? fmaxf(hi4, sc[j]) : __builtin_elementwise_maximum(hi4, sc[j]);
         hi4 += noise_bound(max(max(x.x, x.y), max(x.z, x.w)));
-        if (!__any(!(hi4 + screen_margin(hi4) < floor_w) && hi4 != -INFINITY)) return;
+        if (!__any(!(hi4 + screen_margin(hi4) < floor_w))) return;
         const uint32_t xs[4] = {x.x, x.y, x.z, x.w};
         float floor_t = floor_w;
 #pragma unroll
@@ -208,13 +293,12 @@ DASH_DEV int draw_row(const Draw& a, const float* row, uint32_t step, uint32_t u
             const float sa = sc[j] + cheap_gumbel(xs[j]);
             const float mg = screen_margin(sa);
             if (!(sa + mg < floor_t)) {
-                const float s = (UNIT_T ? l[j] : div_rn(l[j], a.temperature)) + gumbel_from_bits(xs[j]);
-                // indices grow within a thread: the smallest stays on ties, also of quotients that overflow to -inf
-                if (s > best_s || best_i == 0x7FFFFFFF) {
-                    best_s = s;
-                    best_i = i + j;
+                const float e = (UNIT_T ? l[j] : div_rn(l[j], a.temperature)) + gumbel_from_bits(xs[j]);
+                if (better(e, i0 + j, s, i)) {  // (a quotient that overflows to -inf still comes before none)
+                    s = e;
+                    i = i0 + j;
                 }
-                floor_t = fmaxf(floor_t, s);
+                floor_t = fmaxf(floor_t, e);
             } else {
                 floor_t = fmaxf(floor_t, sa - mg);
             }
@@ -222,109 +306,390 @@ DASH_DEV int draw_row(const Draw& a, const float* row, uint32_t step, uint32_t u
         const float f = wave_max_f(floor_t);
         if (f > floor_w && (threadIdx.x & 63) == 0)
             (void)__hip_atomic_fetch_max(floor_s, f, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
-    });
-    return block_best(best_s, best_i, best);
+    }
+};
+
+// HIST: top_p < 1.  MINP: min_p > 0.  SPLIT: stretches of rows, left for draw_join.
+template <bool UNIT_T, bool HIST, bool MINP, bool SPLIT>
+__global__ void __launch_bounds__(kRowThreads, 8)
+draw_first(Draw a, RowSplit cut, FirstPart* __restrict__ part, uint32_t* __restrict__ hists, RowState* __restrict__ state,
+           int* __restrict__ open) {
+    __shared__ uint32_t hist[HIST ? kBins * kCopies : 1];
+    __shared__ BestShared best;
+    __shared__ SettleShared settled;
+    __shared__ float red_f[kRowWaves];
+    __shared__ float floor_s, top_s;
+    __shared__ int far_s;
+    const int b = SPLIT ? blockIdx.x / cut.n : blockIdx.x, n = SPLIT ? blockIdx.x % cut.n : 0;
+    const float* row = a.logits + (int64_t)(a.row_of ? a.row_of[b] : b) * a.ld;
+    Drawing<UNIT_T> draw(a, b, &floor_s);
+    if (threadIdx.x == 0) {
+        top_s = -INFINITY;
+        far_s = 0;
+    }
+    if constexpr (HIST)
+        for (int i = threadIdx.x; i < kBins * kCopies; i += kRowThreads) hist[i] = 0u;
+    __syncthreads();
+    const float min_gap = MINP ? (float)((double)a.temperature * a.log_min_p) : 0.f;
+    const int copy = threadIdx.x & (kCopies - 1);
+    float ref = -FLT_MAX, bins_at = NAN, top = -INFINITY;
+    double z = 0.0;
+    walk_row<4, true, false>(
+        row, SPLIT ? n * cut.len : 0, SPLIT ? min(a.vocab, (n + 1) * cut.len) : a.vocab,
+        [&](const f32x4_t (&buf)[4], int) {
+            // The reference of the sums and of the bins: the largest of a sample of the row.
+            float m = -INFINITY;
+#pragma unroll
+            for (int d = 0; d < 4; ++d)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) m = fmaxf(m, buf[d][j] < INFINITY ? buf[d][j] : -INFINITY);
+            m = block_max_f(m, red_f);
+            if (m == -INFINITY) return;
+            ref = m;
+            if (HIST && fabsf(m * a.scale) < 16384.f) {  // (whole octaves: stretches share a grid of bins)
+                bins_at = rintf(m * a.scale);
+                ref = octaves(bins_at, a.temperature);
+            }
+        },
+        [&](f32x4_t l, int i) {
+            finite_or_low(l);
+            const float m4 = max4(l);
+            if (!__any(m4 > -INFINITY)) return;
+            top = fmaxf(top, m4);
+            const bool far = (m4 - ref) * a.scale >= (HIST ? (float)kBinsAbove : 40.f);
+            if (__any(far)) {  // as in exp_push4; the histogram is void then
+                if (far) {
+                    z *= (double)__builtin_amdgcn_exp2f((ref - m4) * a.scale);
+                    ref = m4;
+                    far_s = 1;
+                }
+            }
+            float e[4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) e[j] = __builtin_amdgcn_exp2f((l[j] - ref) * a.scale);
+            z += (double)((e[0] + e[1]) + (e[2] + e[3]));
+            if constexpr (HIST) {
+#pragma unroll
+                for (int j = 0; j < 4; ++j) atomicAdd(&hist[bin_of(e[j]) * kCopies + copy], bin_term(e[j]));
+            }
+            if constexpr (MINP) {
+                // No entry below the largest logit so far by more than the border's distance can be kept.
+                float top_w = __hip_atomic_load(&top_s, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
+                if (__any(m4 > top_w)) {
+                    top_w = wave_max_f(m4);
+                    if ((threadIdx.x & 63) == 0)
+                        (void)__hip_atomic_fetch_max(&top_s, top_w, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
+                }
+                const float border = top_w + min_gap;
+                const float low = border - fabsf(border) * 1e-6f - fabsf(min_gap) * 1e-6f;  // (not above it by rounding)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) l[j] = l[j] < low ? -INFINITY : l[j];
+                if (!__any(max4(l) > -INFINITY)) return;
+            }
+            draw.score4(a, l, i);
+        },
+        [](int) { return false; });
+    block_best(draw.s, draw.i, best);
+    top = block_max_f(top, red_f);
+    const float at = block_max_f(z > 0.0 ? ref : -FLT_MAX, red_f);
+    const double T = a.temperature;
+    z = block_sum_d(z > 0.0 ? z * exp(((double)ref - (double)at) / T) : 0.0, settled.red);
+    if (far_s) bins_at = NAN;
+    uint32_t bin = 0;
+    if constexpr (HIST) {
+#pragma unroll
+        for (int c = 0; c < kCopies; ++c) bin += hist[threadIdx.x * kCopies + c];
+    }
+    if constexpr (SPLIT) {
+        if (HIST) hists[(int64_t)blockIdx.x * kBins + threadIdx.x] = bin;
+        if (threadIdx.x == 0) part[blockIdx.x] = FirstPart{z, at, top, bins_at, draw.s, draw.i, 0};
+    } else {
+        const double by = exp(((double)at - (double)top) / T);  // sums relative to the largest logit
+        settle(a, b, row, draw.i, top, z * by, bins_at == bins_at ? at : NAN, bin_mass(bin, threadIdx.x) * by, settled, state,
+               open);
+    }
 }
 
-// Mass before w and of the row, relative to the largest logit, in float32 or (EXACT) float64 exponentials.
-template <bool EXACT>
-DASH_DEV void mass_before(const Draw& a, const float* row, const Before& w, float top, double* red, double& before,
-                          double& all) {
-    double sb = 0.0, sa = 0.0;
-    walk_row<4, false>(row, 0, a.vocab, [&](const f32x4_t& l, int i) {
-        if constexpr (EXACT) {
+// Joins the stretches of a row.
+template <bool HIST>
+__global__ void __launch_bounds__(kRowThreads)
+draw_join(Draw a, const FirstPart* __restrict__ part, const uint32_t* __restrict__ hists, int parts,
+          RowState* __restrict__ state, int* __restrict__ open) {
+    __shared__ double bins[HIST ? kBins : 1];
+    __shared__ SettleShared settled;
+    const int b = blockIdx.x, lane = threadIdx.x & 63;
+    const float* row = a.logits + (int64_t)(a.row_of ? a.row_of[b] : b) * a.ld;
+    part += (int64_t)b * parts;
+    FirstPart p{0.0, -FLT_MAX, -INFINITY, NAN, -INFINITY, kNone, 0};
+    if (lane < parts) p = part[lane];
+    float top = p.top, s = p.s, ref = p.z > 0.0 ? p.ref : -FLT_MAX;
+    int tok = p.i;
+    // stretches without an entry have no part in the histogram
+    const bool empty = !(p.z > 0.0);
+    const bool whole = __all(lane >= parts || empty || p.bins_at == p.bins_at);
+    float at = empty || p.bins_at != p.bins_at ? -FLT_MAX : p.bins_at;
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                if (!(fabsf(l[j]) < INFINITY)) continue;
-                const double e = exp(((double)l[j] - (double)top) / (double)a.temperature);
-                sa += e;
-                if (l[j] > w.l || (l[j] == w.l && i + j < w.i)) sb += e;
-            }
-        } else {
-            float ta = 0.f, tb = 0.f;
+    for (int o = 32; o >= 1; o >>= 1) {
+        top = fmaxf(top, __shfl_xor(top, o, 64));
+        ref = fmaxf(ref, __shfl_xor(ref, o, 64));
+        at = fmaxf(at, __shfl_xor(at, o, 64));
+        const float os = __shfl_xor(s, o, 64);
+        const int oi = __shfl_xor(tok, o, 64);
+        if (better(os, oi, s, tok)) {
+            s = os;
+            tok = oi;
+        }
+    }
+    const double T = a.temperature;
+    const double to_ref = p.z > 0.0 ? exp(((double)p.ref - (double)ref) / T) : 0.0;
+    double z = p.z * to_ref;
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const float v = fabsf(l[j]) < INFINITY ? l[j] : -INFINITY;
-                const float e = __builtin_amdgcn_exp2f((v - top) * a.scale);
-                ta += e;
-                tb += v > w.l || (v == w.l && i + j < w.i) ? e : 0.f;
+    for (int o = 32; o >= 1; o >>= 1) z += __shfl_xor(z, o, 64);
+    const double by = exp(((double)ref - (double)top) / T);
+    double bin = 0.0;
+    if constexpr (HIST) {
+        // Bins of all stretches lie on one grid; those that end below the row's lowest bin join it.
+        bins[threadIdx.x] = 0.0;
+        __syncthreads();
+        for (int q = 0; q < parts; ++q) {
+            const float from = __shfl(p.bins_at, q, 64);
+            if (__shfl((int)empty, q, 64) || from != from) continue;
+            const int to = (int)threadIdx.x - (int)fminf((at - from) * (float)kBinsPerOctave, (float)kBins);
+            const double mass = bin_mass(hists[((int64_t)b * parts + q) * kBins + threadIdx.x], threadIdx.x) * __shfl(to_ref, q, 64);
+            if (to >= 0) bins[to] += mass;
+            __syncthreads();
+            if (to < 0 && mass > 0.0) atomicAdd(&bins[0], mass);
+            __syncthreads();
+        }
+        bin = bins[threadIdx.x] * by;
+    }
+    settle(a, b, row, tok, top, z * by, whole ? octaves(at, a.temperature) : NAN, bin, settled, state,
+           open);
+}
+
+// Over entries [lo, hi) of a row: the float32 mass that comes before the winner w.tok, and the draw over
+// what comes before it and can be kept, in every thread.
+template <bool UNIT_T>
+DASH_DEV double draw_before(const Draw& a, int b, const float* row, int lo, int hi, const RowState& w, float* floor_s,
+                            BestShared& best, double* red, float& s, int& tok) {
+    __syncthreads();
+    Drawing<UNIT_T> draw(a, b, floor_s);
+    __syncthreads();
+    double mass = 0.0;
+    // the least exponential of the border's bin (bin 0 holds all below it, too)
+    const float border = w.bin_ref == w.bin_ref && w.border > 0 ? __uint_as_float((kBinBase + w.border) << 18) : 0.f;
+    walk_row<4, false>(row, lo, hi, [&](f32x4_t l, int i) {
+        finite_or_low(l);
+        if (!__any(max4(l) >= w.l)) return;
+        float e[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            l[j] = l[j] > w.l || (l[j] == w.l && i + j < w.tok) ? l[j] : -INFINITY;
+            e[j] = __builtin_amdgcn_exp2f((l[j] - w.top) * a.scale);
+        }
+        mass += (double)((e[0] + e[1]) + (e[2] + e[3]));
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+            l[j] = l[j] < w.low || __builtin_amdgcn_exp2f((l[j] - w.bin_ref) * a.scale) < border ? -INFINITY : l[j];
+        if (__any(max4(l) > -INFINITY)) draw.score4(a, l, i);
+    });
+    s = draw.s;
+    tok = draw.i;
+    block_best(s, tok, best);
+    return block_sum_d(mass, red);
+}
+
+// The rows that are open among rows [first, first + kRowThreads), in order; returns their number.
+DASH_DEV int open_rows(const int* open, int first, int rows, int* list, int* red) {
+    const int r = first + (int)threadIdx.x;
+    const int mine = r < rows && open[r];
+    int total;
+    const int upto = block_scan(mine, red, total);
+    if (mine) list[upto - 1] = r;
+    __syncthreads();
+    return total;
+}
+// Stretches per open row: as many as its chunk of rows leaves work-groups for.
+DASH_DEV int open_cuts(int n, int most) { return max(1, min(most, (int)gridDim.x / max(n, 1))); }
+
+template <bool UNIT_T>
+__global__ void __launch_bounds__(kRowThreads)
+draw_second(Draw a, int rows, const RowState* __restrict__ state, const int* __restrict__ open, int most,
+            SecondPart* __restrict__ second, int* __restrict__ cuts_of) {
+    __shared__ BestShared best;
+    __shared__ double red_d[kRowWaves];
+    __shared__ int list[kRowThreads], red_i[kRowWaves];
+    __shared__ float floor_s;
+    for (int first = 0; first < rows; first += kRowThreads) {
+        __syncthreads();
+        const int n = open_rows(open, first, rows, list, red_i);
+        const int cuts = open_cuts(n, most), len = ((a.vocab + cuts - 1) / cuts + 3) & ~3;
+        for (int item = blockIdx.x; item < n * cuts; item += gridDim.x) {
+            const int b = list[item / cuts], lo = min(a.vocab, item % cuts * len);
+            const float* row = a.logits + (int64_t)(a.row_of ? a.row_of[b] : b) * a.ld;
+            const RowState w = state[b];
+            float s;
+            int tok;
+            const double before = draw_before<UNIT_T>(a, b, row, lo, min(a.vocab, lo + len), w, &floor_s, best, red_d, s, tok);
+            if (threadIdx.x == 0) {
+                second[(int64_t)b * most + item % cuts] = SecondPart{before, s, tok};
+                cuts_of[b] = cuts;  // (the same from every stretch)
             }
-            sa += (double)ta;
-            sb += (double)tb;
+        }
+    }
+}
+
+// Whether the mass before (l, i) is below top_p of the row's, in float64 throughout.
+DASH_DEV bool kept_exactly(const Draw& a, const float* row, float l0, int i0, float top, double* red) {
+    double before = 0.0, all = 0.0;
+    walk_row<2, false>(row, 0, a.vocab, [&](const f32x4_t& l, int i) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            if (!(fabsf(l[j]) < INFINITY)) continue;
+            const double e = exp(((double)l[j] - (double)top) / (double)a.temperature);
+            all += e;
+            if (l[j] > l0 || (l[j] == l0 && i + j < i0)) before += e;
         }
     });
-    before = block_sum_d(sb, red);
-    all = block_sum_d(sa, red);
+    before = block_sum_d(before, red);
+    all = block_sum_d(all, red);
+    return before < a.top_p * all;
 }
 
 template <bool UNIT_T>
 __global__ void __launch_bounds__(kRowThreads)
-draw_top_p(Draw a) {
+draw_last(Draw a, int rows, const RowState* __restrict__ state, const int* __restrict__ open, int most,
+          const SecondPart* __restrict__ second, const int* __restrict__ cuts_of) {
     __shared__ BestShared best;
     __shared__ double red_d[kRowWaves];
-    __shared__ float red_f[kRowWaves];
+    __shared__ int list[kRowThreads], red_i[kRowWaves];
     __shared__ float floor_s;
-    const int b = blockIdx.x;
-    const float* row = a.logits + (int64_t)(a.row_of ? a.row_of[b] : b) * a.ld;
-    const uint32_t step = (uint32_t)a.step[b], uid = (uint32_t)a.uid[b];
-    const double T = a.temperature;
-    Before w{INFINITY, 0x7FFFFFFF, -INFINITY};
-    ExpSum sum;
-    float top = -INFINITY;
-    int tok = draw_row<UNIT_T, true>(a, row, step, uid, w, &floor_s, best, sum, top);
-    if (tok == 0x7FFFFFFF) {
-        if (threadIdx.x == 0) write_draw(a, b, -1, 0.0);
-        return;
-    }
-    top = block_max_f(top, red_f);
-    const double z = block_sum_d(sum.z * exp(((double)sum.ref - (double)top) / T), red_d);
-    {  // the least float at or above the min-p border
-        const double t = (double)top + T * a.log_min_p;
-        w.low = (float)t;
-        if ((double)w.low < t) w.low = nextafterf(w.low, INFINITY);
-    }
-    for (;;) {
-        w.l = row[tok];
-        w.i = tok;
-        bool kept = w.l >= w.low;
-        if (kept && a.top_p < 1.0) {
-            // all but the winner's own mass is at least what comes before it
-            const double own = exp(((double)w.l - (double)top) / T) / z;
-            if (!(1.0 - own < a.top_p - kMassTol)) {
-                double before, all;
-                mass_before<false>(a, row, w, top, red_d, before, all);
-                if (fabs(before - a.top_p * all) <= kMassTol * all) mass_before<true>(a, row, w, top, red_d, before, all);
-                kept = before < a.top_p * all;
+    for (int first = 0; first < rows; first += kRowThreads) {
+        __syncthreads();
+        const int n = open_rows(open, first, rows, list, red_i);
+        for (int item = blockIdx.x; item < n; item += gridDim.x) {
+            const int b = list[item], cuts = cuts_of[b], lane = threadIdx.x & 63;
+            const float* row = a.logits + (int64_t)(a.row_of ? a.row_of[b] : b) * a.ld;
+            RowState w = state[b];
+            double before = 0.0;
+            float s = -INFINITY;
+            int next = kNone;
+            if (lane < cuts) {
+                const SecondPart p = second[(int64_t)b * most + lane];
+                before = p.before;
+                s = p.s;
+                next = p.i;
             }
+#pragma unroll
+            for (int o = 32; o >= 1; o >>= 1) {
+                before += __shfl_xor(before, o, 64);
+                const float os = __shfl_xor(s, o, 64);
+                const int oi = __shfl_xor(next, o, 64);
+                if (better(os, oi, s, next)) {
+                    s = os;
+                    next = oi;
+                }
+            }
+            for (;;) {
+                bool kept = false;
+                if (w.unsure) {
+                    kept = before < a.top_p * w.z;
+                    if (fabs(before - a.top_p * w.z) <= kMassTol * w.z) kept = kept_exactly(a, row, w.l, w.tok, w.top, red_d);
+                }
+                if (kept || next == kNone) break;  // (the first token of the order is kept: there is a next one)
+                w.tok = next;
+                w.l = row[next];
+                if (a.top_p >= 1.0 || kept_by_own_mass(a, w.l, w.top, w.z)) break;
+                if (w.bin_ref == w.bin_ref && bin_of(__builtin_amdgcn_exp2f((w.l - w.bin_ref) * a.scale)) >= w.sure) break;
+                w.unsure = 1;
+                before = draw_before<UNIT_T>(a, b, row, 0, a.vocab, w, &floor_s, best, red_d, s, next);
+            }
+            if (threadIdx.x == 0) write_draw(a, b, w.tok, ((double)w.l - (double)w.top) / (double)a.temperature - log(w.z));
         }
-        if (kept) break;
-        tok = draw_row<UNIT_T, false>(a, row, step, uid, w, &floor_s, best, sum, top);
-        if (tok == 0x7FFFFFFF) break;  // (the first token of the order is always kept)
     }
-    if (threadIdx.x == 0) {
-        if (tok == 0x7FFFFFFF) write_draw(a, b, -1, 0.0);
-        else write_draw(a, b, tok, ((double)row[tok] - (double)top) / T - log(z));
-    }
+}
+
+constexpr int kMostParts = 16;  // stretches of a row in the first pass: draw_join reads a histogram of each
+constexpr int kMostCuts = 64;   // in the second: a wave joins them
+struct DrawPlan {
+    RowSplit first;
+    int most;  // room for stretches of the second pass, per row
+    size_t hists, parts, states, seconds, opens, bytes;  // offsets in the workspace
+};
+DrawPlan draw_plan(int rows, int vocab) {
+    DrawPlan p;
+    const int n = std::max(rows, 1);
+    p.first = split_row(vocab, std::min({kMostParts, kDrawTarget / n, vocab / kDrawStretch}));
+    p.most = std::max(1, std::min({kMostCuts, std::max(kDrawTarget / n, 8), vocab / kDrawStretch}));
+    const size_t stretches = p.first.n > 1 ? (size_t)n * p.first.n : 0;
+    size_t at = 0;
+    auto take = [&](size_t bytes) {
+        const size_t here = at;
+        at += (bytes + 15) / 16 * 16;
+        return here;
+    };
+    p.hists = take(stretches * kBins * sizeof(uint32_t));
+    p.parts = take(stretches * sizeof(FirstPart));
+    p.states = take(n * sizeof(RowState));
+    p.seconds = take((size_t)n * p.most * sizeof(SecondPart));
+    p.opens = take(2 * (size_t)n * sizeof(int));
+    p.bytes = at;
+    return p;
 }
 
 }  // namespace
 
+size_t sample_truncated_workspace_bytes(int rows, int vocab, int top_k) {
+    if (top_k > 0 && top_k < vocab) return top_workspace_bytes(rows, vocab, top_k);
+    return draw_plan(rows, vocab).bytes;
+}
+
 hipError_t launch_sample_truncated(const float* logits, int64_t ld, int rows, int vocab, const int32_t* row_of,
                                    const int32_t* uid, const int32_t* step, float temperature, int top_k, double top_p,
                                    double min_p, uint64_t seed, int32_t* tok_out, float* lp_out, uint32_t* status,
-                                   hipStream_t st) {
+                                   void* ws, hipStream_t st) {
     if (rows <= 0) return hipSuccess;
     const Draw a{logits, ld, vocab, row_of, uid, step, temperature, exp2_scale(temperature), top_k, top_p,
                  log(min_p), (uint32_t)seed, (uint32_t)(seed >> 32), tok_out, lp_out, status};
-    const bool unit = temperature == 1.0f;
-    if (top_k > 0 && top_k < vocab) {
-        if (unit) draw_top_k<true><<<rows, kRowThreads, 0, st>>>(a);
-        else draw_top_k<false><<<rows, kRowThreads, 0, st>>>(a);
-    } else {
-        if (unit) draw_top_p<true><<<rows, kRowThreads, 0, st>>>(a);
-        else draw_top_p<false><<<rows, kRowThreads, 0, st>>>(a);
-    }
-    return hipGetLastError();
+    auto launch = [&](auto unit) -> hipError_t {
+        constexpr bool U = decltype(unit)::value;
+        if (top_k > 0 && top_k < vocab) {
+            TopParts parts;
+            if (hipError_t e = launch_top_parts(logits, ld, rows, vocab, row_of, top_k, temperature,
+                                                top_plan(rows, vocab, top_k), ws, parts, st))
+                return e;
+            draw_top_k<U><<<rows, kRowThreads, 0, st>>>(a, parts);
+            return hipGetLastError();
+        }
+        const DrawPlan p = draw_plan(rows, vocab);
+        char* at = (char*)ws;
+        uint32_t* hists = (uint32_t*)(at + p.hists);
+        FirstPart* parts = (FirstPart*)(at + p.parts);
+        RowState* state = (RowState*)(at + p.states);
+        SecondPart* second = (SecondPart*)(at + p.seconds);
+        int* open = (int*)(at + p.opens);
+        int* cuts_of = open + rows;
+        auto first = [&](auto hist, auto minp) {
+            constexpr bool H = decltype(hist)::value, M = decltype(minp)::value;
+            if (p.first.n == 1) {
+                draw_first<U, H, M, false><<<rows, kRowThreads, 0, st>>>(a, p.first, parts, hists, state, open);
+            } else {
+                draw_first<U, H, M, true><<<rows * p.first.n, kRowThreads, 0, st>>>(a, p.first, parts, hists, state, open);
+                draw_join<H><<<rows, kRowThreads, 0, st>>>(a, parts, hists, p.first.n, state, open);
+            }
+        };
+        const bool hist = top_p < 1.0 && vocab <= kHistVocab;
+        if (hist && min_p > 0.0) first(std::true_type{}, std::true_type{});
+        else if (hist) first(std::true_type{}, std::false_type{});
+        else if (min_p > 0.0) first(std::false_type{}, std::true_type{});
+        else first(std::false_type{}, std::false_type{});
+        if (top_p < 1.0 || min_p > 0.0) {  // (otherwise every row has ended)
+            draw_second<U><<<kDrawTarget, kRowThreads, 0, st>>>(a, rows, state, open, p.most, second, cuts_of);
+            draw_last<U><<<std::min(rows, kDrawTarget), kRowThreads, 0, st>>>(a, rows, state, open, p.most, second, cuts_of);
+        }
+        return hipGetLastError();
+    };
+    return temperature == 1.0f ? launch(std::true_type{}) : launch(std::false_type{});
 }
 
 }  // namespace dash

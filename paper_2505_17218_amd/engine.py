@@ -181,6 +181,14 @@ def _ld(t: torch.Tensor) -> int:
     return t.stride(0) if t.shape[0] > 1 else t.shape[1]
 
 
+def _room(nbytes: int, device):
+    """(workspace tensor to hold on to, its aligned address or None, its bytes)."""
+    if nbytes == 0:
+        return None, None, 0
+    ws = torch.empty(nbytes + 256, dtype=torch.uint8, device=device)
+    return ws, aligned(ws), nbytes
+
+
 def sample_truncated(logits: torch.Tensor, seq_uid: torch.Tensor, step: torch.Tensor, temperature: float, seed: int,
                      top_k: int = 0, top_p: float = 1.0, min_p: float = 0.0, row_of: torch.Tensor | None = None,
                      with_logprob: bool = True, status: torch.Tensor | None = None):
@@ -195,9 +203,10 @@ def sample_truncated(logits: torch.Tensor, seq_uid: torch.Tensor, step: torch.Te
     toks = torch.empty(n, dtype=torch.int32, device=logits.device)
     lps = torch.empty(n, dtype=torch.float32, device=logits.device) if with_logprob else None
     if n:
+        ws, at, size = _room(L.dash_sample_truncated_workspace_bytes(n, logits.shape[1], top_k), logits.device)
         L.dash_sample_truncated(logits.data_ptr(), _ld(logits), n, logits.shape[1], L.ptr(row_of), seq_uid.data_ptr(),
                                 step.data_ptr(), temperature, top_k, top_p, min_p, seed, toks.data_ptr(), L.ptr(lps),
-                                L.ptr(status), stream_handle())
+                                L.ptr(status), at, size, stream_handle())
     return toks, lps
 
 
@@ -210,8 +219,9 @@ def top_logits(logits: torch.Tensor, k: int, temperature: float = 1.0):
     indices = torch.empty(rows, max(k, 0), dtype=torch.int32, device=logits.device)
     rest = torch.empty(rows, dtype=torch.float32, device=logits.device)
     if rows:
+        ws, at, size = _room(L.dash_top_logits_workspace_bytes(rows, V, k), logits.device)
         L.dash_top_logits(logits.data_ptr(), _ld(logits), rows, V, k, temperature, values.data_ptr(),
-                          indices.data_ptr(), rest.data_ptr(), stream_handle())
+                          indices.data_ptr(), rest.data_ptr(), at, size, stream_handle())
     return values, indices, rest
 
 
@@ -244,8 +254,9 @@ def distill_loss(logits: torch.Tensor, values: torch.Tensor, indices: torch.Tens
     loss = torch.empty(rows, dtype=torch.float32, device=logits.device)
     norm = torch.empty(rows, 4, dtype=torch.float32, device=logits.device)
     if rows:
+        ws, at, size = _room(L.dash_distill_workspace_bytes(rows, V), logits.device)
         L.dash_distill_loss(logits.data_ptr(), _ld(logits), rows, V, values.data_ptr(), indices.data_ptr(),
-                            L.ptr(rest), k, temperature, loss.data_ptr(), norm.data_ptr(), stream_handle())
+                            L.ptr(rest), k, temperature, loss.data_ptr(), norm.data_ptr(), at, size, stream_handle())
     return loss, norm
 
 
@@ -272,9 +283,10 @@ def distill_loss_grad(logits: torch.Tensor, values: torch.Tensor, indices: torch
     out, code = _grad_buffer(logits, out, dtype)
     loss = torch.empty(rows, dtype=torch.float32, device=logits.device)
     if rows:
+        ws, at, size = _room(L.dash_distill_workspace_bytes(rows, V), logits.device)
         L.dash_distill_loss_grad(logits.data_ptr(), _ld(logits), rows, V, values.data_ptr(), indices.data_ptr(),
                                  L.ptr(rest), k, temperature, L.ptr(weight), loss.data_ptr(), out.data_ptr(), _ld(out),
-                                 code, stream_handle())
+                                 code, at, size, stream_handle())
     return loss, out
 
 

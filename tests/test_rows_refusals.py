@@ -20,8 +20,10 @@ def _status(f, *args):
     return e.value.status
 
 
-def _sample(logits=BIG, ld=512, n=4, V=512, uid=0x2000, step=0x3000, T=1.0, top_k=5, top_p=0.9, min_p=0.0, out=0x4000):
-    L.dash_sample_truncated(logits, ld, n, V, None, uid, step, T, top_k, top_p, min_p, 1, out, None, None, None)
+def _sample(logits=BIG, ld=512, n=4, V=512, uid=0x2000, step=0x3000, T=1.0, top_k=5, top_p=0.9, min_p=0.0, out=0x4000,
+            ws=0x10000, ws_bytes=1 << 30):
+    L.dash_sample_truncated(logits, ld, n, V, None, uid, step, T, top_k, top_p, min_p, 1, out, None, None, ws, ws_bytes,
+                            None)
 
 
 @pytest.mark.parametrize("bad", [dict(logits=None), dict(uid=None), dict(step=None), dict(out=None), dict(n=-1),
@@ -37,10 +39,16 @@ def test_sample_truncated_limits():
     assert _status(lambda: _sample(top_k=1025, V=4096, ld=4096)) == L.DASH_ENOTSUP
     assert _status(lambda: _sample(n=(1 << 21) + 1)) == L.DASH_ENOTSUP
     _sample(n=0)  # no rows: nothing to do
+    need = L.dash_sample_truncated_workspace_bytes(4, 151936, 0)
+    assert need > 0
+    for ws, size in ((None, need), (0x10000, need - 1), (0x10000, 0)):
+        assert _status(lambda: _sample(V=151936, ld=151936, top_k=0, ws=ws, ws_bytes=size)) == L.DASH_ECAPACITY
+    assert _status(lambda: _sample(V=151936, ld=151936, top_k=0, ws=0x10080)) == L.DASH_EINVAL
 
 
-def _top(logits=BIG, ld=512, rows=4, V=512, k=8, T=1.0, values=0x2000, indices=0x3000):
-    L.dash_top_logits(logits, ld, rows, V, k, T, values, indices, None, None)
+def _top(logits=BIG, ld=512, rows=4, V=512, k=8, T=1.0, values=0x2000, indices=0x3000,
+         ws=0x10000, ws_bytes=1 << 30):
+    L.dash_top_logits(logits, ld, rows, V, k, T, values, indices, None, ws, ws_bytes, None)
 
 
 @pytest.mark.parametrize("bad, want", [
@@ -53,16 +61,34 @@ def test_top_logits_refuses(bad, want):
     _top(rows=0)
 
 
+def test_workspaces_that_are_too_small():
+    need = L.dash_top_logits_workspace_bytes(1, 151936, 64)
+    assert need > 0 and L.dash_top_logits_workspace_bytes(5000, 151936, 64) == 0
+    for ws, size in ((None, need), (0x10000, need - 1)):
+        assert _status(lambda: _top(rows=1, V=151936, ld=151936, k=64, ws=ws, ws_bytes=size)) == L.DASH_ECAPACITY
+    assert _status(lambda: _top(rows=1, V=151936, ld=151936, k=64, ws=0x10010)) == L.DASH_EINVAL
+    need = L.dash_distill_workspace_bytes(1, 151936)
+    assert need > 0 and L.dash_distill_workspace_bytes(5000, 151936) == 0
+    for f in (_loss, _both):
+        a = _args(rows=1, V=151936, ld=151936, ldg=151936)
+        assert _status(f, {**a, "ws_bytes": need - 1}) == L.DASH_ECAPACITY
+        assert _status(f, {**a, "ws": None}) == L.DASH_ECAPACITY
+        assert _status(f, {**a, "ws": 0x10010}) == L.DASH_EINVAL
+    # sizes that the calls refuse need none
+    assert L.dash_top_logits_workspace_bytes(0, 100, 5) == L.dash_top_logits_workspace_bytes(1, 100, 0) == 0
+    assert L.dash_sample_truncated_workspace_bytes(-1, 100, 5) == L.dash_distill_workspace_bytes(3, 0) == 0
+
+
 def _args(**kw):
     a = dict(logits=BIG, ld=512, rows=4, V=512, val=0x2000, idx=0x3000, rest=None, k=8, T=1.0, loss=0x4000, norm=0x5000,
-             weight=None, grad=0x20000000, ldg=512, dtype=0)
+             weight=None, grad=0x20000000, ldg=512, dtype=0, ws=0x10000, ws_bytes=1 << 30)
     a.update(kw)
     return a
 
 
 def _loss(a):
     L.dash_distill_loss(a["logits"], a["ld"], a["rows"], a["V"], a["val"], a["idx"], a["rest"], a["k"], a["T"],
-                        a["loss"], a["norm"], None)
+                        a["loss"], a["norm"], a["ws"], a["ws_bytes"], None)
 
 
 def _grad(a):
@@ -72,7 +98,7 @@ def _grad(a):
 
 def _both(a):
     L.dash_distill_loss_grad(a["logits"], a["ld"], a["rows"], a["V"], a["val"], a["idx"], a["rest"], a["k"], a["T"],
-                             a["weight"], a["loss"], a["grad"], a["ldg"], a["dtype"], None)
+                             a["weight"], a["loss"], a["grad"], a["ldg"], a["dtype"], a["ws"], a["ws_bytes"], None)
 
 
 COMMON = [(dict(logits=None), 1), (dict(val=None), 1), (dict(idx=None), 1), (dict(rows=-1), 1), (dict(V=0), 1),
