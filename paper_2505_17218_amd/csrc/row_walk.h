@@ -10,9 +10,11 @@
 
 namespace dash {
 
+// Threads of a work-group (NT below) unless a kernel says otherwise, and its waves.
 constexpr int kRowThreads = 1024;
 constexpr int kRowWaves = kRowThreads / 64;
-constexpr int kRowTile = 4 * kRowThreads;  // entries of one step: four consecutive ones per thread
+// Entries of one step of NT threads, a tile: four consecutive ones per thread.
+constexpr int kRowTile = 4 * kRowThreads;
 
 // Rows start on any float: gfx950 loads 16 bytes from a 4-byte aligned address in one instruction.
 typedef float f32x4u_t __attribute__((ext_vector_type(4), aligned(4)));
@@ -34,10 +36,11 @@ DASH_DEV f32x4_t load_row4(const float* row, int i) {
 // these before f does; where there are fewer whole tiles than DEPTH, the last one (the partial one,
 // if there is none) fills the places of the missing.  round(t) is called after the t-th DEPTH tiles
 // (1, 2, ...) and ends the walk by returning true.  STREAM: rows that nothing reads again.
-template <int DEPTH, bool STRIPES, bool STREAM, class START, class F, class ROUND>
+template <int DEPTH, bool STRIPES, bool STREAM, int NT = kRowThreads, class START, class F, class ROUND>
 DASH_DEV void walk_row(const float* __restrict__ row, int lo, int hi, START&& start, F&& f, ROUND&& round) {
-    const int whole = (hi - lo) / kRowTile;
-    const int end = lo + whole * kRowTile, at = lo + 4 * (int)threadIdx.x;
+    constexpr int kTile = 4 * NT;
+    const int whole = (hi - lo) / kTile;
+    const int end = lo + whole * kTile, at = lo + 4 * (int)threadIdx.x;
     f32x4_t last = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
     if (end < hi) {  // the partial tile is loaded first and used last
         const int i = end + 4 * (int)threadIdx.x;
@@ -54,20 +57,20 @@ DASH_DEV void walk_row(const float* __restrict__ row, int lo, int hi, START&& st
         };
         f32x4_t buf[DEPTH];
 #pragma unroll
-        for (int d = 0; d < DEPTH; ++d) buf[d] = load_row4<STREAM>(row, at + tile(0, d) * kRowTile);
+        for (int d = 0; d < DEPTH; ++d) buf[d] = load_row4<STREAM>(row, at + tile(0, d) * kTile);
         start(buf, whole);
         for (int t = 0; t < rounds; ++t) {
 #pragma unroll
             for (int d = 0; d < DEPTH; ++d) {
-                f(buf[d], at + tile(t, d) * kRowTile);
-                buf[d] = load_row4<STREAM>(row, at + tile(t + 1, d) * kRowTile);
+                f(buf[d], at + tile(t, d) * kTile);
+                buf[d] = load_row4<STREAM>(row, at + tile(t + 1, d) * kTile);
             }
             if (round(t + 1)) return;
         }
 #pragma unroll
         for (int d = 0; d < DEPTH - 1; ++d) {
             if (d >= left) break;
-            f(buf[d], at + tile(rounds, d) * kRowTile);
+            f(buf[d], at + tile(rounds, d) * kTile);
         }
     } else {
         f32x4_t buf[DEPTH];
@@ -77,9 +80,9 @@ DASH_DEV void walk_row(const float* __restrict__ row, int lo, int hi, START&& st
     }
     if (end < hi) f(last, end + 4 * (int)threadIdx.x);
 }
-template <int DEPTH, bool STREAM, class F>
+template <int DEPTH, bool STREAM, int NT = kRowThreads, class F>
 DASH_DEV void walk_row(const float* __restrict__ row, int lo, int hi, F&& f) {
-    walk_row<DEPTH, false, STREAM>(row, lo, hi, [](const f32x4_t (&)[DEPTH], int) {}, (F&&)f, [](int) { return false; });
+    walk_row<DEPTH, false, STREAM, NT>(row, lo, hi, [](const f32x4_t (&)[DEPTH], int) {}, (F&&)f, [](int) { return false; });
 }
 
 // Rows cut into n stretches of len entries (the last one shorter, none empty; len a multiple of four),
@@ -132,8 +135,17 @@ DASH_DEV void exp_push4(ExpSum& s, const f32x4_t& x, float m4, float scale, floa
     s.z += (double)((e[0] + e[1]) + (e[2] + e[3]));
 }
 
-// Inclusive sum over the threads up to this one (of kRowThreads), and the total.
-template <class T>
+// One finite term.
+DASH_DEV void exp_push1(ExpSum& s, float x, float scale) {
+    if (x > s.ref) {
+        s.z *= (double)__builtin_amdgcn_exp2f((s.ref - x) * scale);
+        s.ref = x;
+    }
+    s.z += (double)__builtin_amdgcn_exp2f((x - s.ref) * scale);
+}
+
+// Inclusive sum over the threads up to this one (of NT), and the total.
+template <int NT = kRowThreads, class T>
 DASH_DEV T block_scan(T v, T* red, T& total) {
     const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
 #pragma unroll
@@ -145,23 +157,23 @@ DASH_DEV T block_scan(T v, T* red, T& total) {
     if (lane == 63) red[w] = v;
     __syncthreads();
     // every wave sums the waves' totals, a lane each
-    T t = lane < kRowWaves ? red[lane] : (T)0;
+    T t = lane < NT / 64 ? red[lane] : (T)0;
 #pragma unroll
-    for (int o = 1; o < kRowWaves; o <<= 1) {
+    for (int o = 1; o < NT / 64; o <<= 1) {
         const T u = __shfl_up(t, o, 64);
         if (lane >= o) t += u;
     }
-    total = __shfl(t, kRowWaves - 1, 64);
+    total = __shfl(t, NT / 64 - 1, 64);
     const T before = __shfl(t, max(w - 1, 0), 64);
     return v + (w ? before : (T)0);
 }
 
 DASH_DEV float max4(const f32x4_t& x) { return fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])); }
 
-// Reductions over the work-group's kRowThreads threads in a fixed order; every thread gets the
-// result.  `red` is scratch of kRowWaves values that no other reduction is using: consecutive
+// Reductions over the work-group's NT threads in a fixed order; every thread gets the
+// result.  `red` is scratch of NT / 64 values that no other reduction is using: consecutive
 // reductions through one scratch are separated by their own leading barrier.
-template <class T, class OP>
+template <int NT = kRowThreads, class T, class OP>
 DASH_DEV T block_reduce(T v, T* red, OP op) {
 #pragma unroll
     for (int o = 32; o >= 1; o >>= 1) v = op(v, (T)__shfl_xor(v, o, 64));
@@ -170,21 +182,24 @@ DASH_DEV T block_reduce(T v, T* red, OP op) {
     __syncthreads();
     T s = red[0];
 #pragma unroll
-    for (int i = 1; i < kRowWaves; ++i) s = op(s, red[i]);
+    for (int i = 1; i < NT / 64; ++i) s = op(s, red[i]);
     return s;
 }
+template <int NT = kRowThreads>
 DASH_DEV double block_sum_d(double v, double* red) {
-    return block_reduce(v, red, [](double a, double b) { return a + b; });
+    return block_reduce<NT>(v, red, [](double a, double b) { return a + b; });
 }
+template <int NT = kRowThreads>
 DASH_DEV float block_max_f(float v, float* red) {
-    return block_reduce(v, red, [](float a, float b) { return fmaxf(a, b); });
+    return block_reduce<NT>(v, red, [](float a, float b) { return fmaxf(a, b); });
 }
 
 // Sum over the work-group's threads of e^((l - ref) / T) (0: nothing), and ref.
+template <int NT = kRowThreads>
 DASH_DEV double block_exp_sum(const ExpSum& s, double temperature, float* red_f, double* red_d, float& ref) {
-    ref = block_max_f(s.z > 0.0 ? s.ref : -FLT_MAX, red_f);
+    ref = block_max_f<NT>(s.z > 0.0 ? s.ref : -FLT_MAX, red_f);
     // (a NaN sum stays one)
-    return block_sum_d(s.z == 0.0 ? 0.0 : s.z * exp(((double)s.ref - (double)ref) / temperature), red_d);
+    return block_sum_d<NT>(s.z == 0.0 ? 0.0 : s.z * exp(((double)s.ref - (double)ref) / temperature), red_d);
 }
 
 }  // namespace dash

@@ -9,9 +9,10 @@
 // cuts below in it, its loop reloaded spilled addresses, and every such reload waits for all loads
 // in flight.
 //
-// The second gathers a row's lists in LDS, cuts them to the K largest and sorts those.  A list that
-// overflowed (a row that holds one value many times, or whose large values the sample misses) sends
-// it over the row itself, with a cut whenever the next tile might not fit.  That is slower, never wrong.
+// The second reads a row's lists into registers, cuts them to the K largest and sorts those in LDS.
+// Lists that do not fit are cut piece by piece, and one that overflowed (a row that holds one value
+// many times, or whose large values the sample misses) sends it over the row itself, a cut whenever
+// the next tile might not fit.  That is slower, never wrong.
 //
 // Entries are held as one 64-bit word, key(l) : ~index, where key orders floats as unsigned
 // integers: a larger word is a larger logit, or an equal one at a lower index, and no two are equal.
@@ -24,8 +25,6 @@
 namespace dash {
 
 constexpr int kTopMax = 1024;             // largest K: one sorted entry per thread
-constexpr int kTopCap = 2 * kRowTile;     // words in LDS: 64 KB, two work-groups per CU
-constexpr int kTopPer = kTopCap / kRowThreads;
 constexpr int kTopStart = 4;              // tiles that give the bound
 constexpr float kEvictOne = 17592186044416.f;  // 2^44: evicted terms are summed as integers of 2^-44
 
@@ -65,24 +64,28 @@ struct TopParts {
 hipError_t launch_top_parts(const float* logits, int64_t ld, int rows, int vocab, const int32_t* row_of, int k,
                             float temperature, const TopPlan& plan, void* ws, TopParts& out, hipStream_t st);
 
+constexpr int kBoundParts = 1024;
+template <int NT>
 struct BoundShared {
-    int hist[kRowThreads];
+    int hist[kBoundParts];
     int found[3];
-    int red_i[kRowWaves];
+    int red[NT / 64];
 };
 
 // A bound b with k <= (words e at or above b), and at most k + slack unless equal words straddle that;
 // lo <= b < hi, count words are at or above lo, none at or above hi.  The first `per` of a thread's
 // words count.  A histogram of the range in 1024 parts, summed from the top, finds the part that holds
 // the k-th word; that part is the range of the next round, if it holds too many.  Two rounds as a rule.
-template <class W, int PER>
-DASH_DEV W top_bound(BoundShared& sh, const W (&e)[PER], int per, int k, int slack, W lo, W hi, int& count) {
+template <int NT, class W, int PER>
+DASH_DEV W top_bound(BoundShared<NT>& sh, const W (&e)[PER], int per, int k, int slack, W lo, W hi, int& count) {
+    constexpr int kOwn = kBoundParts / NT;  // parts per thread, from the top
     int above = 0;  // words at or above hi
     while (count > k + slack && hi - lo > 1) {
         const int bits = (int)(8 * sizeof(uint64_t)) - __clzll((unsigned long long)(hi - lo - 1));
         const int shift = max(bits - 10, 0);
         __syncthreads();
-        sh.hist[threadIdx.x] = 0;
+#pragma unroll
+        for (int q = 0; q < kOwn; ++q) sh.hist[threadIdx.x + q * NT] = 0;
         __syncthreads();
 #pragma unroll
         for (int r = 0; r < PER; ++r) {
@@ -90,13 +93,19 @@ DASH_DEV W top_bound(BoundShared& sh, const W (&e)[PER], int per, int k, int sla
             if (e[r] >= lo && e[r] < hi) atomicAdd(&sh.hist[(int)((e[r] - lo) >> shift)], 1);
         }
         __syncthreads();
-        const int part = kRowThreads - 1 - (int)threadIdx.x, here = sh.hist[part];
-        int total;
-        const int upto = above + block_scan(here, sh.red_i, total);
-        if (upto >= k && upto - here < k) {
-            sh.found[0] = part;
-            sh.found[1] = upto;
-            sh.found[2] = upto - here;
+        const int first = kBoundParts - 1 - kOwn * (int)threadIdx.x;
+        int here[kOwn], sum = 0, total;
+#pragma unroll
+        for (int q = 0; q < kOwn; ++q) sum += here[q] = sh.hist[first - q];
+        int upto = above + block_scan<NT>(sum, sh.red, total) - sum;  // words above this thread's parts
+#pragma unroll
+        for (int q = 0; q < kOwn; ++q) {
+            if (upto < k && upto + here[q] >= k) {
+                sh.found[0] = first - q;
+                sh.found[1] = upto + here[q];
+                sh.found[2] = upto;
+            }
+            upto += here[q];
         }
         __syncthreads();
         lo += (W)sh.found[0] << shift;
@@ -108,48 +117,49 @@ DASH_DEV W top_bound(BoundShared& sh, const W (&e)[PER], int per, int k, int sla
     return lo;
 }
 
-// ---- the second launch: a row's words in LDS ---------------------------------------------------
+// ---- the second launch -----------------------------------------------------------------------------
 
+// A work-group of NT threads holds NT PER words: 256 x 16 for K up to 256, where several rows share a
+// CU and a barrier is of four waves; 1024 x 8 above.
+constexpr int kTopSmall = 256;
+template <int NT, int PER>
 struct TopShared {
-    uint64_t c[kTopCap];
+    uint64_t c[NT * PER];
     uint64_t evict_z;
     int count;         // words appended
     unsigned evict_ref;
     int kept;
-    BoundShared bound;
-    double red_d[kRowWaves];
-    float red_f[kRowWaves];
+    int at[64];        // where the words of each list begin
+    BoundShared<NT> bound;
+    double red_d[NT / 64];
+    float red_f[NT / 64];
 };
+constexpr int kTopParts = 64;  // stretches of a row at most (a wave adds up their lists)
 // Uniform over the work-group but for `rest`.
 struct TopState {
-    int n = 0;       // words in the buffer, as of the last barrier that counted
+    int n = 0;         // words in LDS, as of the last barrier that counted
     uint64_t low = 0;  // words must reach this
-    ExpSum rest;     // the thread's share of the entries that were turned away
+    ExpSum rest;       // the thread's share of the entries that were turned away
 };
 
-// Cuts the buffer from n > k + slack words to k .. k + slack; what falls out joins the rest, and the
-// bound rises to the least word left.  Between barriers that separate it from appends.
-DASH_DEV void top_cut(TopShared& sh, TopState& st, int k, int slack, float scale) {
-    const int per = (st.n + kRowThreads - 1) / kRowThreads;
-    uint64_t e[kTopPer];
-#pragma unroll
-    for (int r = 0; r < kTopPer; ++r) {
-        const int i = r * kRowThreads + (int)threadIdx.x;
-        e[r] = i < st.n ? sh.c[i] : 0;
-    }
-    int count = st.n;
-    const uint64_t b = top_bound(sh.bound, e, per, k, slack, (uint64_t)kKeyLowest << 32, (uint64_t)kKeyInf << 32, count);
+// Of n words in the threads' registers (word r NT + thread is e[r]; 0: none) those at or above a bound
+// that leaves k .. k + slack of them (all, if n is no more) go to LDS, the others join the rest.
+template <int NT, int PER>
+DASH_DEV void top_keep(TopShared<NT, PER>& sh, TopState& st, const uint64_t (&e)[PER], int n, int k, int slack, float scale) {
+    const int per = (n + NT - 1) / NT;
+    int count = n;
+    const uint64_t b = top_bound<NT>(sh.bound, e, per, k, slack, (uint64_t)kKeyLowest << 32, (uint64_t)kKeyInf << 32, count);
+    __syncthreads();  // every word is in a register
     if (threadIdx.x == 0) {
         sh.evict_z = 0;
         sh.evict_ref = 0;
         sh.kept = 0;
     }
-    __syncthreads();  // every word is in a register
+    __syncthreads();
     unsigned out = 0;  // the largest key that falls out
 #pragma unroll
-    for (int r = 0; r < kTopPer; ++r) {
-        if (r >= per) break;
-        const uint64_t keep = __ballot(e[r] >= b);
+    for (int r = 0; r < PER; ++r) {
+        const uint64_t keep = r < per ? __ballot(e[r] >= b) : 0;
         if (keep) {
             int at = 0;
             if ((threadIdx.x & 63) == 0) at = atomicAdd(&sh.kept, __popcll(keep));
@@ -158,7 +168,11 @@ DASH_DEV void top_cut(TopShared& sh, TopState& st, int k, int slack, float scale
         }
         if (e[r] && e[r] < b) out = max(out, (unsigned)(e[r] >> 32));
     }
-    if (out) atomicMax(&sh.evict_ref, out);
+    if (__any(out != 0)) {
+#pragma unroll
+        for (int o = 32; o >= 1; o >>= 1) out = max(out, (unsigned)__shfl_xor((int)out, o, 64));
+        if ((threadIdx.x & 63) == 0) atomicMax(&sh.evict_ref, out);
+    }
     __syncthreads();
     // Integer terms relative to the largest: their sum does not depend on the order of the words,
     // which varies with the order in which waves appended them.
@@ -167,11 +181,15 @@ DASH_DEV void top_cut(TopShared& sh, TopState& st, int k, int slack, float scale
         const float ref = top_value(top);
         uint64_t z = 0;
 #pragma unroll
-        for (int r = 0; r < kTopPer; ++r) {
+        for (int r = 0; r < PER; ++r) {
             if (r >= per) break;
             if (e[r] && e[r] < b) z += (uint64_t)(__builtin_amdgcn_exp2f((word_value(e[r]) - ref) * scale) * kEvictOne);
         }
-        if (z) atomicAdd((unsigned long long*)&sh.evict_z, (unsigned long long)z);
+        if (__any(z != 0)) {
+#pragma unroll
+            for (int o = 32; o >= 1; o >>= 1) z += (uint64_t)__shfl_xor((long long)z, o, 64);
+            if ((threadIdx.x & 63) == 0) atomicAdd((unsigned long long*)&sh.evict_z, (unsigned long long)z);
+        }
         __syncthreads();
         if (threadIdx.x == 0) {
             const double zd = (double)sh.evict_z / (double)kEvictOne;
@@ -186,11 +204,24 @@ DASH_DEV void top_cut(TopShared& sh, TopState& st, int k, int slack, float scale
     if (threadIdx.x == 0) sh.count = count;
     st.n = count;
     st.low = b;
+}
+
+// Cuts the words in LDS to k .. k + slack.
+template <int NT, int PER>
+DASH_DEV void top_cut(TopShared<NT, PER>& sh, TopState& st, int k, int slack, float scale) {
+    uint64_t e[PER];
+#pragma unroll
+    for (int r = 0; r < PER; ++r) {
+        const int i = r * NT + (int)threadIdx.x;
+        e[r] = i < st.n ? sh.c[i] : 0;
+    }
+    top_keep(sh, st, e, st.n, k, slack, scale);
     __syncthreads();
 }
 
-// Appends the words of those lanes that have one (any lanes of a wave).
-DASH_DEV void top_append(TopShared& sh, bool mine, uint64_t word) {
+// Appends the words of those lanes that have one.
+template <int NT, int PER>
+DASH_DEV void top_append(TopShared<NT, PER>& sh, bool mine, uint64_t word) {
     const uint64_t in = __ballot(mine);
     if (!in) return;
     int at = 0;
@@ -198,80 +229,124 @@ DASH_DEV void top_append(TopShared& sh, bool mine, uint64_t word) {
     at = __builtin_amdgcn_readfirstlane(at);
     if (mine) sh.c[at + __popcll(in & ((1ull << (threadIdx.x & 63)) - 1))] = word;
 }
-// After at most kRowTile appends: room for as many again.
-DASH_DEV void top_count(TopShared& sh, TopState& st, int k, float scale) {
-    __syncthreads();
-    st.n = sh.count;
-    __syncthreads();
-    if (st.n > kTopCap - kRowTile) top_cut(sh, st, k, (k >> 2) + 32, scale);
-}
 
-// The words of row b among them the k largest, and the rest of the row.
-DASH_DEV void top_gather(TopShared& sh, TopState& st, const TopParts& p, int64_t b, const float* row, int vocab, int k,
-                         float scale) {
-    if (threadIdx.x == 0) sh.count = 0;
-    const TopPart* part = p.part + b * p.n;
-    const uint64_t* words = p.words + b * p.n * p.room;
-    bool fits = true;
-    if ((int)threadIdx.x < p.n) {
-        const TopPart mine = part[threadIdx.x];
-        fits = mine.n <= p.room;
-        if (mine.z > 0.0) {
+// Leaves the k largest words of row b in LDS, at most p >= k of them (st.n), unsorted, and the row's
+// other entries in the rest.
+template <int NT, int PER>
+DASH_DEV void top_gather(TopShared<NT, PER>& sh, TopState& st, const TopParts& parts, int64_t b, const float* row,
+                         int vocab, int k, int p, float scale) {
+    constexpr int kCap = NT * PER, kTile = 4 * NT;
+    const TopPart* part = parts.part + b * parts.n;
+    const uint64_t* words = parts.words + b * parts.n * parts.room;
+    const int lane = threadIdx.x & 63;
+    // every wave adds up the lists
+    int n = 0;
+    if (lane < parts.n) {
+        const TopPart mine = part[lane];
+        n = mine.n;
+        if (threadIdx.x < 64 && mine.z > 0.0) {
             st.rest.ref = mine.ref;
             st.rest.z = mine.z;
         }
     }
-    if (__syncthreads_and(fits)) {
-        for (int from = 0; from < p.n * p.room; from += kRowTile) {  // (room is a multiple of 64: a wave has one list)
+    const bool fits = __all(n <= parts.room);
+    int upto = n;
 #pragma unroll
-            for (int r = 0; r < kRowTile / kRowThreads; ++r) {
-                const int i = from + r * kRowThreads + (int)threadIdx.x;
-                if (i >= p.n * p.room) break;
-                const bool in = i % p.room < part[i / p.room].n;
-                top_append(sh, in, in ? words[i] : 0);
-            }
-            top_count(sh, st, k, scale);
+    for (int o = 1; o < 64; o <<= 1) {
+        const int u = __shfl_up(upto, o, 64);
+        if (lane >= o) upto += u;
+    }
+    const int total = __shfl(upto, 63, 64);
+    if (threadIdx.x < 64) sh.at[lane] = upto - n;
+    if (threadIdx.x == 0) sh.count = 0;
+    __syncthreads();
+    auto word = [&](int i) {  // the i-th of all lists
+        int s = 0;
+        if (parts.n > 1) {
+#pragma unroll
+            for (int o = 32; o >= 1; o >>= 1)
+                if (s + o < parts.n && sh.at[s + o] <= i) s += o;
         }
+        return words[(int64_t)s * parts.room + i - sh.at[s]];
+    };
+    if (fits && total <= kCap) {
+        uint64_t e[PER];
+#pragma unroll
+        for (int r = 0; r < PER; ++r) {
+            const int i = r * NT + (int)threadIdx.x;
+            e[r] = i < total ? word(i) : 0;
+        }
+        top_keep(sh, st, e, total, k, total > p ? p - k : total, scale);
+        __syncthreads();
         return;
     }
-    st = TopState{};
-    for (int at = 0; at < vocab; at += kRowTile) {
-        walk_row<1, true>(row, at, min(vocab, at + kRowTile), [&](f32x4_t l, int i) {
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const bool entry = fabsf(l[j]) < INFINITY;
-                const uint64_t w = entry ? top_word(l[j], i + j) : 0;
-                const bool in = entry && w >= st.low;
-                top_append(sh, in, w);
-                if (in || !entry) l[j] = -INFINITY;
+    const int slack = (k >> 2) + 32;
+    auto count = [&] {  // after at most kTile appends: room for as many again
+        __syncthreads();
+        st.n = sh.count;
+        __syncthreads();
+        if (st.n > kCap - kTile) top_cut(sh, st, k, slack, scale);
+    };
+    if (fits) {
+        for (int from = 0; from < total; from += kTile) {
+#pragma unroll 1
+            for (int i = from + (int)threadIdx.x; i - lane < min(total, from + kTile); i += NT) {
+                const uint64_t w = i < total ? word(i) : 0;
+                top_append(sh, w >= max(st.low, (uint64_t)1), w);
+                if (w && w < st.low) {
+                    const float l = word_value(w);
+                    exp_push1(st.rest, l, scale);
+                }
             }
-            exp_push4<false>(st.rest, l, max4(l), scale);
-        });
-        top_count(sh, st, k, scale);
+            count();
+        }
+    } else {
+        st = TopState{};
+#pragma unroll 1
+        for (int at = 0; at < vocab; at += kTile) {
+            walk_row<1, true, NT>(row, at, min(vocab, at + kTile), [&](f32x4_t l, int i) {
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const bool entry = fabsf(l[j]) < INFINITY;
+                    const uint64_t w = entry ? top_word(l[j], i + j) : 0;
+                    const bool in = entry && w >= st.low;
+                    top_append(sh, in, w);
+                    if (in || !entry) l[j] = -INFINITY;
+                }
+                exp_push4<false>(st.rest, l, max4(l), scale);
+            });
+            count();
+        }
     }
+    if (st.n > p) top_cut(sh, st, k, p - k, scale);
 }
 
-// Leaves the m = min(n, k) largest words sorted in sh.c[0 .. m), descending (what lies behind them in
-// the buffer is added to the rest); returns m.
-DASH_DEV int top_finish(TopShared& sh, TopState& st, int k, float scale) {
+// Words that a row's selection leaves at most: sorting pads to it.
+DASH_DEV int top_room(int k) {
     int p = 64;
     while (p < k) p <<= 1;
-    __syncthreads();
-    if (st.n > p) top_cut(sh, st, k, p - k, scale);
+    return p;
+}
+
+// Sorts the st.n <= p words in LDS, descending; those behind the first m = min(n, k), which it returns,
+// join the rest.
+template <int NT, int PER>
+DASH_DEV int top_finish(TopShared<NT, PER>& sh, TopState& st, int k, int p, float scale) {
     const int n = st.n;
-    for (int i = n + (int)threadIdx.x; i < p; i += kRowThreads) sh.c[i] = 0;
+    for (int i = n + (int)threadIdx.x; i < p; i += NT) sh.c[i] = 0;
     __syncthreads();
-    if (p <= 128) {
+    if constexpr (NT <= kTopSmall) {
         // A word's place is the number of larger ones (words differ; zeros fill what is left):
-        // kRowThreads / p threads per word count over a share of the words each.
-        const int i = (int)threadIdx.x & (p - 1), share = (int)threadIdx.x / p, len = p * p / kRowThreads;
+        // NT / p threads per word count over a share of the words each.
+        const int i = (int)threadIdx.x & (p - 1), share = (int)threadIdx.x / p, len = p * p / NT;
         const uint64_t mine = sh.c[i];
         int place = 0;
+#pragma unroll 8
         for (int j = share * len; j < (share + 1) * len; ++j) place += sh.c[j] > mine;
         sh.bound.hist[threadIdx.x] = place;
         __syncthreads();
         if ((int)threadIdx.x < p) {
-            for (int q = 1; q < kRowThreads / p; ++q) place += sh.bound.hist[threadIdx.x + q * p];
+            for (int q = 1; q < NT / p; ++q) place += sh.bound.hist[threadIdx.x + q * p];
             if (mine) sh.c[place] = mine;  // (each thread has its own word in a register)
         }
     } else {
@@ -291,12 +366,8 @@ DASH_DEV int top_finish(TopShared& sh, TopState& st, int k, float scale) {
         }
     }
     __syncthreads();
-    const int m = min(n, k);
-    const int i = m + (int)threadIdx.x;
-    if (__any(i < n)) {
-        const float l = i < n ? word_value(sh.c[i]) : -INFINITY;
-        exp_push4<false>(st.rest, f32x4_t{l, -INFINITY, -INFINITY, -INFINITY}, l, scale);
-    }
+    const int m = min(n, k), i = m + (int)threadIdx.x;  // (n - m <= p - k < NT)
+    if (i < n) exp_push1(st.rest, word_value(sh.c[i]), scale);
     return m;
 }
 

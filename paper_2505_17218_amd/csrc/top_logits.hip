@@ -7,12 +7,12 @@ namespace dash {
 
 namespace {
 
-constexpr int kTopTarget = 512, kTopStretch = 4096, kTopParts = 64, kTopRoom = 16384;
+constexpr int kTopTarget = 512, kTopStretch = 4096, kTopRoom = 16384;
 
 __global__ void __launch_bounds__(kRowThreads, 8)
 top_part_k(const float* __restrict__ logits, int64_t ld, int vocab, const int32_t* __restrict__ row_of, int k,
            double temperature, float scale, TopPlan plan, TopPart* __restrict__ part, uint64_t* __restrict__ words) {
-    __shared__ BoundShared bound;
+    __shared__ BoundShared<kRowThreads> bound;
     __shared__ int count;
     __shared__ double red_d[kRowWaves];
     __shared__ float red_f[kRowWaves];
@@ -40,7 +40,7 @@ top_part_k(const float* __restrict__ logits, int64_t ld, int vocab, const int32_
             }
             int n = kTopStart / 2 * kRowThreads;
             // (no bound where the sample holds fewer than k entries)
-            const uint32_t low = top_bound(bound, e, kTopStart / 2, k, k >> 3, 0u, kKeyInf, n);
+            const uint32_t low = top_bound<kRowThreads>(bound, e, kTopStart / 2, k, k >> 3, 0u, kKeyInf, n);
             if (low >= kKeyLowest) thr = value_below(low);
             thr = __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(thr)));
         },
@@ -76,14 +76,16 @@ top_part_k(const float* __restrict__ logits, int64_t ld, int vocab, const int32_
     if (threadIdx.x == 0) part[blockIdx.x] = TopPart{z, ref, count};
 }
 
-__global__ void __launch_bounds__(kRowThreads)
+template <int NT, int PER>
+__global__ void __launch_bounds__(NT)
 top_logits_k(const float* __restrict__ logits, int64_t ld, int vocab, int k, double temperature, float scale,
              TopParts parts, float* __restrict__ values, int32_t* __restrict__ indices, float* __restrict__ rest) {
-    __shared__ TopShared sh;
+    __shared__ TopShared<NT, PER> sh;
     const int64_t r = blockIdx.x;
     TopState st;
-    top_gather(sh, st, parts, r, logits + r * ld, vocab, k, scale);
-    const int m = top_finish(sh, st, k, scale);
+    const int p = top_room(k);
+    top_gather(sh, st, parts, r, logits + r * ld, vocab, k, p, scale);
+    const int m = top_finish(sh, st, k, p, scale);
     if ((int)threadIdx.x < k) {
         const bool some = (int)threadIdx.x < m;
         const uint64_t w = some ? sh.c[threadIdx.x] : 0;
@@ -92,7 +94,7 @@ top_logits_k(const float* __restrict__ logits, int64_t ld, int vocab, int k, dou
     }
     if (!rest) return;
     float ref;
-    const double z = block_exp_sum(st.rest, temperature, sh.red_f, sh.red_d, ref);
+    const double z = block_exp_sum<NT>(st.rest, temperature, sh.red_f, sh.red_d, ref);
     if (threadIdx.x == 0) rest[r] = z > 0.0 ? (float)((double)ref / temperature + log(z)) : -INFINITY;
 }
 
@@ -133,8 +135,11 @@ hipError_t launch_top_logits(const float* logits, int64_t ld, int rows, int voca
     TopParts p;
     if (hipError_t e = launch_top_parts(logits, ld, rows, vocab, nullptr, k, temperature, top_plan(rows, vocab, k), ws, p, st))
         return e;
-    top_logits_k<<<rows, kRowThreads, 0, st>>>(logits, ld, vocab, k, (double)temperature, exp2_scale(temperature), p,
-                                               values, indices, rest);
+    const float scale = exp2_scale(temperature);
+    if (k <= kTopSmall)
+        top_logits_k<256, 16><<<rows, 256, 0, st>>>(logits, ld, vocab, k, (double)temperature, scale, p, values, indices, rest);
+    else
+        top_logits_k<1024, 8><<<rows, 1024, 0, st>>>(logits, ld, vocab, k, (double)temperature, scale, p, values, indices, rest);
     return hipGetLastError();
 }
 

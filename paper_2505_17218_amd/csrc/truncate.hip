@@ -79,6 +79,7 @@ struct BestShared {
     float s[kRowWaves];
     int i[kRowWaves];
 };
+template <int NT = kRowThreads>
 DASH_DEV void block_best(float& s, int& i, BestShared& sh) {
 #pragma unroll
     for (int o = 32; o >= 1; o >>= 1) {
@@ -98,32 +99,33 @@ DASH_DEV void block_best(float& s, int& i, BestShared& sh) {
     s = sh.s[0];
     i = sh.i[0];
 #pragma unroll
-    for (int w = 1; w < kRowWaves; ++w)
+    for (int w = 1; w < NT / 64; ++w)
         if (better(sh.s[w], sh.i[w], s, i)) {
             s = sh.s[w];
             i = sh.i[w];
         }
 }
 
-template <bool UNIT_T>
-__global__ void __launch_bounds__(kRowThreads)
+template <bool UNIT_T, int NT, int PER>
+__global__ void __launch_bounds__(NT)
 draw_top_k(Draw a, TopParts parts) {
-    __shared__ TopShared sh;
+    __shared__ TopShared<NT, PER> sh;
     __shared__ BestShared best;
     const int b = blockIdx.x;
     const float* row = a.logits + (int64_t)(a.row_of ? a.row_of[b] : b) * a.ld;
     TopState st;
-    top_gather(sh, st, parts, b, row, a.vocab, a.top_k, a.scale);
-    const int m = top_finish(sh, st, a.top_k, a.scale);
+    const int p = top_room(a.top_k);
+    top_gather(sh, st, parts, b, row, a.vocab, a.top_k, p, a.scale);
+    const int m = top_finish(sh, st, a.top_k, p, a.scale);
     const double T = a.temperature;
     float ref;
-    const double rest = block_exp_sum(st.rest, T, sh.red_f, sh.red_d, ref);
+    const double rest = block_exp_sum<NT>(st.rest, T, sh.red_f, sh.red_d, ref);
     const bool in = (int)threadIdx.x < m;
     const uint64_t word = in ? sh.c[threadIdx.x] : 0;
     const float l = word_value(word), l0 = word_value(sh.c[0]);
     const double w = in ? exp(((double)l - (double)l0) / T) : 0.0;
     double total;
-    const double upto = block_scan(w, sh.red_d, total);
+    const double upto = block_scan<NT>(w, sh.red_d, total);
     bool keep = in && (a.top_p >= 1.0 || upto - w < a.top_p * total);
     keep = keep && (double)l >= (double)l0 + T * a.log_min_p;
     float s = -INFINITY;
@@ -132,7 +134,7 @@ draw_top_k(Draw a, TopParts parts) {
         tok = word_index(word);
         s = (UNIT_T ? l : div_rn(l, a.temperature)) + noise_of(a, tok, (uint32_t)a.step[b], (uint32_t)a.uid[b]);
     }
-    block_best(s, tok, best);
+    block_best<NT>(s, tok, best);
     if (threadIdx.x != 0) return;
     if (tok == kNone) {
         write_draw(a, b, -1, 0.0);
@@ -157,11 +159,12 @@ constexpr int kBinsBelow = 20, kBinsAbove = kBins / kBinsPerOctave - kBinsBelow;
 constexpr uint32_t kBinBase = (127 - kBinsBelow) * kBinsPerOctave;
 constexpr int kCopies = 4;
 constexpr int kHistVocab = 1 << 18;
+constexpr int kMostParts = 16;  // stretches of a row in the first pass: draw_join reads a histogram of each
 constexpr double kBinTol = 1.3e-4;  // 2^-13, rounded up
 DASH_DEV int bin_of(float e) { return min(max((int)(__float_as_uint(e) >> 18) - (int)kBinBase, 0), kBins - 1); }
 DASH_DEV uint32_t bin_term(float e) { return __builtin_amdgcn_ubfe(__float_as_uint(e), 10, 13) | 0x2000u; }
 // Value of a sum of terms of bin i.  (Entries below the lowest bin join it and count for more than they
-// are; that moves only the mass at or above bin 0, which rules nothing out and settles nothing.)
+// are, or are left out; that moves only the mass at or above bin 0, which rules nothing out and settles nothing.)
 DASH_DEV double bin_mass(uint32_t sum, int i) { return ldexp((double)sum, i / kBinsPerOctave - kBinsBelow - 13); }
 
 // What a work-group that walked a stretch of a row in draw_first leaves.
@@ -222,8 +225,8 @@ DASH_DEV void settle(const Draw& a, int b, const float* row, int tok, float top,
                 const double below = block_scan(bin, sh.red, all);
                 const double from = all - below + bin, tol = (kMassTol + kBinTol) * z;
                 auto most = [](int x, int y) { return max(x, y); };
-                const int last = block_reduce(from >= a.top_p * z - tol ? (int)threadIdx.x : -kBins, sh.red_i, most);
-                const int whole = block_reduce(from >= a.top_p * z + tol ? (int)threadIdx.x : -kBins, sh.red_i, most);
+                const int last = block_reduce(from >= a.top_p * z - tol ? (int)threadIdx.x : 0, sh.red_i, most);
+                const int whole = block_reduce(from >= a.top_p * z + tol ? (int)threadIdx.x : 0, sh.red_i, most);
                 r.sure = last + 2;
                 r.border = whole - 1;
                 const int at = bin_of(__builtin_amdgcn_exp2f((r.l - bin_ref) * a.scale));
@@ -415,7 +418,6 @@ template <bool HIST>
 __global__ void __launch_bounds__(kRowThreads)
 draw_join(Draw a, const FirstPart* __restrict__ part, const uint32_t* __restrict__ hists, int parts,
           RowState* __restrict__ state, int* __restrict__ open) {
-    __shared__ double bins[HIST ? kBins : 1];
     __shared__ SettleShared settled;
     const int b = blockIdx.x, lane = threadIdx.x & 63;
     const float* row = a.logits + (int64_t)(a.row_of ? a.row_of[b] : b) * a.ld;
@@ -448,20 +450,20 @@ draw_join(Draw a, const FirstPart* __restrict__ part, const uint32_t* __restrict
     const double by = exp(((double)ref - (double)top) / T);
     double bin = 0.0;
     if constexpr (HIST) {
-        // Bins of all stretches lie on one grid; those that end below the row's lowest bin join it.
-        bins[threadIdx.x] = 0.0;
-        __syncthreads();
-        for (int q = 0; q < parts; ++q) {
-            const float from = __shfl(p.bins_at, q, 64);
-            if (__shfl((int)empty, q, 64) || from != from) continue;
-            const int to = (int)threadIdx.x - (int)fminf((at - from) * (float)kBinsPerOctave, (float)kBins);
-            const double mass = bin_mass(hists[((int64_t)b * parts + q) * kBins + threadIdx.x], threadIdx.x) * __shfl(to_ref, q, 64);
-            if (to >= 0) bins[to] += mass;
-            __syncthreads();
-            if (to < 0 && mass > 0.0) atomicAdd(&bins[0], mass);
-            __syncthreads();
+        // Bins of all stretches lie on one grid; what lies below the row's lowest bin is left out.
+        uint32_t sum[kMostParts];
+        int from[kMostParts];
+#pragma unroll
+        for (int q = 0; q < kMostParts; ++q) {
+            const float theirs = __shfl(p.bins_at, q, 64);
+            from[q] = kBins;
+            if (q < parts && !__shfl((int)empty, q, 64) && theirs == theirs)
+                from[q] = (int)threadIdx.x + (int)fminf((at - theirs) * (float)kBinsPerOctave, (float)kBins);
+            sum[q] = from[q] < kBins ? hists[((int64_t)b * parts + q) * kBins + from[q]] : 0;
         }
-        bin = bins[threadIdx.x] * by;
+#pragma unroll
+        for (int q = 0; q < kMostParts; ++q) bin += bin_mass(sum[q], from[q]) * __shfl(to_ref, q, 64);
+        bin *= by;
     }
     settle(a, b, row, tok, top, z * by, whole ? octaves(at, a.temperature) : NAN, bin, settled, state,
            open);
@@ -609,7 +611,6 @@ draw_last(Draw a, int rows, const RowState* __restrict__ state, const int* __res
     }
 }
 
-constexpr int kMostParts = 16;  // stretches of a row in the first pass: draw_join reads a histogram of each
 constexpr int kMostCuts = 64;   // in the second: a wave joins them
 struct DrawPlan {
     RowSplit first;
@@ -658,7 +659,8 @@ hipError_t launch_sample_truncated(const float* logits, int64_t ld, int rows, in
             if (hipError_t e = launch_top_parts(logits, ld, rows, vocab, row_of, top_k, temperature,
                                                 top_plan(rows, vocab, top_k), ws, parts, st))
                 return e;
-            draw_top_k<U><<<rows, kRowThreads, 0, st>>>(a, parts);
+            if (top_k <= kTopSmall) draw_top_k<U, 256, 16><<<rows, 256, 0, st>>>(a, parts);
+            else draw_top_k<U, 1024, 8><<<rows, 1024, 0, st>>>(a, parts);
             return hipGetLastError();
         }
         const DrawPlan p = draw_plan(rows, vocab);

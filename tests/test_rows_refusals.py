@@ -63,7 +63,7 @@ def test_top_logits_refuses(bad, want):
 
 def test_workspaces_that_are_too_small():
     need = L.dash_top_logits_workspace_bytes(1, 151936, 64)
-    assert need > 0 and L.dash_top_logits_workspace_bytes(5000, 151936, 64) == 0
+    assert need > 0
     for ws, size in ((None, need), (0x10000, need - 1)):
         assert _status(lambda: _top(rows=1, V=151936, ld=151936, k=64, ws=ws, ws_bytes=size)) == L.DASH_ECAPACITY
     assert _status(lambda: _top(rows=1, V=151936, ld=151936, k=64, ws=0x10010)) == L.DASH_EINVAL
