@@ -286,25 +286,26 @@ struct Drawing {
         for (int j = 1; j < 4; ++j) hi4 = UNIT_T ? fmaxf(hi4, sc[j]) : __builtin_elementwise_maximum(hi4, sc[j]);
         hi4 += noise_bound(max(max(x.x, x.y), max(x.z, x.w)));
         if (!__any(!(hi4 + screen_margin(hi4) < floor_w))) return;
+        // Cheap scores of all four first, and the bound from the wave's best of them: then hardly any
+        // lane evaluates an exact score, also while the bound is still low.
         const uint32_t xs[4] = {x.x, x.y, x.z, x.w};
-        float floor_t = floor_w;
+        float up[4], floor_t = floor_w;
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-            if (l[j] == -INFINITY) continue;
-            const float hi = sc[j] + noise_bound(xs[j]);
-            if (hi + screen_margin(hi) < floor_t) continue;
-            const float sa = sc[j] + cheap_gumbel(xs[j]);
-            const float mg = screen_margin(sa);
-            if (!(sa + mg < floor_t)) {
-                const float e = (UNIT_T ? l[j] : div_rn(l[j], a.temperature)) + gumbel_from_bits(xs[j]);
-                if (better(e, i0 + j, s, i)) {  // (a quotient that overflows to -inf still comes before none)
-                    s = e;
-                    i = i0 + j;
-                }
-                floor_t = fmaxf(floor_t, e);
-            } else {
-                floor_t = fmaxf(floor_t, sa - mg);
+            const float sa = sc[j] + cheap_gumbel(xs[j]), mg = screen_margin(sa);
+            up[j] = sa + mg;
+            floor_t = fmaxf(floor_t, l[j] == -INFINITY ? -INFINITY : sa - mg);  // (NaN raises nothing)
+        }
+        floor_t = wave_max_f(floor_t);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            if (l[j] == -INFINITY || up[j] < floor_t) continue;
+            const float e = (UNIT_T ? l[j] : div_rn(l[j], a.temperature)) + gumbel_from_bits(xs[j]);
+            if (better(e, i0 + j, s, i)) {  // (a quotient that overflows to -inf still comes before none)
+                s = e;
+                i = i0 + j;
             }
+            floor_t = fmaxf(floor_t, e);
         }
         const float f = wave_max_f(floor_t);
         if (f > floor_w && (threadIdx.x & 63) == 0)
