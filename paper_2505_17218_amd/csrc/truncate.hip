@@ -146,13 +146,12 @@ draw_top_k(Draw a, TopParts parts) {
 
 // ---- without top-k ----------------------------------------------------------------------------
 
-// ---- without top-k ----------------------------------------------------------------------------
-
 // Histogram of a row's mass: an exponential e relative to a reference logit falls into the part that
 // its exponent and the five bits below it name; there are 1024, one per thread, from 20 octaves
-// below the reference to 12 above (an entry further above voids the histogram).  A part is summed in integers, the leading 14 bits of each e, so
-// sums do not depend on order: 2^18 terms fit, and what is cut off is less than 2^-13 of each.
-// (Float atomics in LDS took five times as long as everything else.)  Lanes add to four copies.
+// below the reference to 12 above (an entry further above voids the histogram).  A part is summed in
+// integers, the leading 14 bits of each e, so sums do not depend on order: 2^18 terms fit, and what is
+// cut off is less than 2^-13 of each.  (Float atomics in LDS took five times as long as everything
+// else.)  Lanes add to four copies.
 constexpr int kBins = kRowThreads;
 constexpr int kBinsPerOctave = 32;
 constexpr int kBinsBelow = 20, kBinsAbove = kBins / kBinsPerOctave - kBinsBelow;  // octaves
@@ -242,12 +241,14 @@ DASH_DEV void settle(const Draw& a, int b, const float* row, int tok, float top,
     else write_draw(a, b, tok, ((double)r.l - (double)top) / (double)a.temperature - log(z));
 }
 
-// Replaces what is no entry by -inf.  A finite sum of the four shows that all are.
-DASH_DEV void finite_or_low(f32x4_t& l) {
-    if (__any(!(fabsf((l[0] + l[1]) + (l[2] + l[3])) < INFINITY))) {
+// Replaces what is no entry by -inf; whether the wave held such.  A finite sum of the four shows that all are.
+DASH_DEV bool finite_or_low(f32x4_t& l) {
+    const bool some = __any(!(fabsf((l[0] + l[1]) + (l[2] + l[3])) < INFINITY));
+    if (some) {
 #pragma unroll
         for (int j = 0; j < 4; ++j) l[j] = fabsf(l[j]) < INFINITY ? l[j] : -INFINITY;
     }
+    return some;
 }
 
 // The draw over a stretch of a row, screened as in sampler.hip: thread and work-group state.
@@ -266,8 +267,8 @@ struct Drawing {
         inv_t = UNIT_T ? 1.f : div_rn(1.f, a.temperature);
         if (threadIdx.x == 0) *floor_s = -INFINITY;
     }
-    // Entries i0 .. i0+3; those that are -inf take no part.
-    DASH_DEV void score4(const Draw& a, const f32x4_t& l, int i0) {
+    // Entries i0 .. i0+3; those that are -inf (only if masked) take no part.
+    DASH_DEV void score4(const Draw& a, const f32x4_t& l, int i0, bool masked) {
         // Relaxed: a stale bound is a lower one, and only more entries are evaluated.
         const float floor_w = __hip_atomic_load(floor_s, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
         uint32_t k0 = a.k0, k1 = a.k1;
@@ -277,35 +278,38 @@ struct Drawing {
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
             // l / T by a product and one corrected step, within the margin of the exact quotient, or
-            // NaN where something overflows (then nothing is screened; so too for an entry of -inf)
+            // NaN where something overflows (then nothing is screened)
             const float q = l[j] * inv_t;
             sc[j] = UNIT_T ? l[j] : __builtin_fmaf(__builtin_fmaf(-q, a.temperature, l[j]), inv_t, q);
+        }
+        if (!UNIT_T && masked) {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) sc[j] = l[j] == -INFINITY ? -INFINITY : sc[j];
         }
         float hi4 = sc[0];
 #pragma unroll
         for (int j = 1; j < 4; ++j) hi4 = UNIT_T ? fmaxf(hi4, sc[j]) : __builtin_elementwise_maximum(hi4, sc[j]);
         hi4 += noise_bound(max(max(x.x, x.y), max(x.z, x.w)));
-        if (!__any(!(hi4 + screen_margin(hi4) < floor_w))) return;
-        // Cheap scores of all four first, and the bound from the wave's best of them: then hardly any
-        // lane evaluates an exact score, also while the bound is still low.
+        if (!__any(!(hi4 + screen_margin(hi4) < floor_w) && hi4 != -INFINITY)) return;
         const uint32_t xs[4] = {x.x, x.y, x.z, x.w};
-        float up[4], floor_t = floor_w;
+        float floor_t = floor_w;
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-            const float sa = sc[j] + cheap_gumbel(xs[j]), mg = screen_margin(sa);
-            up[j] = sa + mg;
-            floor_t = fmaxf(floor_t, l[j] == -INFINITY ? -INFINITY : sa - mg);  // (NaN raises nothing)
-        }
-        floor_t = wave_max_f(floor_t);
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            if (l[j] == -INFINITY || up[j] < floor_t) continue;
-            const float e = (UNIT_T ? l[j] : div_rn(l[j], a.temperature)) + gumbel_from_bits(xs[j]);
-            if (better(e, i0 + j, s, i)) {  // (a quotient that overflows to -inf still comes before none)
-                s = e;
-                i = i0 + j;
+            if (l[j] == -INFINITY) continue;
+            const float hi = sc[j] + noise_bound(xs[j]);
+            if (hi + screen_margin(hi) < floor_t) continue;
+            const float sa = sc[j] + cheap_gumbel(xs[j]);
+            const float mg = screen_margin(sa);
+            if (!(sa + mg < floor_t)) {
+                const float e = (UNIT_T ? l[j] : div_rn(l[j], a.temperature)) + gumbel_from_bits(xs[j]);
+                if (better(e, i0 + j, s, i)) {  // (a quotient that overflows to -inf still comes before none)
+                    s = e;
+                    i = i0 + j;
+                }
+                floor_t = fmaxf(floor_t, e);
+            } else {
+                floor_t = fmaxf(floor_t, sa - mg);
             }
-            floor_t = fmaxf(floor_t, e);
         }
         const float f = wave_max_f(floor_t);
         if (f > floor_w && (threadIdx.x & 63) == 0)
@@ -356,7 +360,7 @@ draw_first(Draw a, RowSplit cut, FirstPart* __restrict__ part, uint32_t* __restr
             }
         },
         [&](f32x4_t l, int i) {
-            finite_or_low(l);
+            bool masked = finite_or_low(l);
             const float m4 = max4(l);
             if (!__any(m4 > -INFINITY)) return;
             top = fmaxf(top, m4);
@@ -389,8 +393,9 @@ draw_first(Draw a, RowSplit cut, FirstPart* __restrict__ part, uint32_t* __restr
 #pragma unroll
                 for (int j = 0; j < 4; ++j) l[j] = l[j] < low ? -INFINITY : l[j];
                 if (!__any(max4(l) > -INFINITY)) return;
+                masked = true;
             }
-            draw.score4(a, l, i);
+            draw.score4(a, l, i, masked);
         },
         [](int) { return false; });
     block_best(draw.s, draw.i, best);
@@ -472,7 +477,7 @@ draw_join(Draw a, const FirstPart* __restrict__ part, const uint32_t* __restrict
 
 // Over entries [lo, hi) of a row: the float32 mass that comes before the winner w.tok, and the draw over
 // what comes before it and can be kept, in every thread.
-template <bool UNIT_T>
+template <int NT, bool UNIT_T>
 DASH_DEV double draw_before(const Draw& a, int b, const float* row, int lo, int hi, const RowState& w, float* floor_s,
                             BestShared& best, double* red, float& s, int& tok) {
     __syncthreads();
@@ -481,7 +486,7 @@ DASH_DEV double draw_before(const Draw& a, int b, const float* row, int lo, int 
     double mass = 0.0;
     // the least exponential of the border's bin (bin 0 holds all below it, too)
     const float border = w.bin_ref == w.bin_ref && w.border > 0 ? __uint_as_float((kBinBase + w.border) << 18) : 0.f;
-    walk_row<4, false>(row, lo, hi, [&](f32x4_t l, int i) {
+    walk_row<2, false, NT>(row, lo, hi, [&](f32x4_t l, int i) {
         finite_or_low(l);
         if (!__any(max4(l) >= w.l)) return;
         float e[4];
@@ -494,21 +499,28 @@ DASH_DEV double draw_before(const Draw& a, int b, const float* row, int lo, int 
 #pragma unroll
         for (int j = 0; j < 4; ++j)
             l[j] = l[j] < w.low || __builtin_amdgcn_exp2f((l[j] - w.bin_ref) * a.scale) < border ? -INFINITY : l[j];
-        if (__any(max4(l) > -INFINITY)) draw.score4(a, l, i);
+        if (__any(max4(l) > -INFINITY)) draw.score4(a, l, i, true);
     });
     s = draw.s;
     tok = draw.i;
-    block_best(s, tok, best);
-    return block_sum_d(mass, red);
+    block_best<NT>(s, tok, best);
+    return block_sum_d<NT>(mass, red);
 }
 
-// The rows that are open among rows [first, first + kRowThreads), in order; returns their number.
+// The later passes have work-groups of kLater threads: with 1024 the last one needed more registers than
+// there are, and a launch with scratch memory took 20 us with nothing to do.  They take rows by chunks.
+constexpr int kLater = 512, kChunk = 1024;
+// The rows that are open among rows [first, first + kChunk), in order; returns their number.
 DASH_DEV int open_rows(const int* open, int first, int rows, int* list, int* red) {
-    const int r = first + (int)threadIdx.x;
-    const int mine = r < rows && open[r];
-    int total;
-    const int upto = block_scan(mine, red, total);
-    if (mine) list[upto - 1] = r;
+    constexpr int kOwn = kChunk / kLater;
+    const int r = first + kOwn * (int)threadIdx.x;
+    int mine[kOwn], sum = 0, total;
+#pragma unroll
+    for (int o = 0; o < kOwn; ++o) sum += mine[o] = r + o < rows && open[r + o];
+    int at = block_scan<kLater>(sum, red, total) - sum;
+#pragma unroll
+    for (int o = 0; o < kOwn; ++o)
+        if (mine[o]) list[at++] = r + o;
     __syncthreads();
     return total;
 }
@@ -516,14 +528,14 @@ DASH_DEV int open_rows(const int* open, int first, int rows, int* list, int* red
 DASH_DEV int open_cuts(int n, int most) { return max(1, min(most, (int)gridDim.x / max(n, 1))); }
 
 template <bool UNIT_T>
-__global__ void __launch_bounds__(kRowThreads)
+__global__ void __launch_bounds__(kLater)
 draw_second(Draw a, int rows, const RowState* __restrict__ state, const int* __restrict__ open, int most,
             SecondPart* __restrict__ second, int* __restrict__ cuts_of) {
     __shared__ BestShared best;
-    __shared__ double red_d[kRowWaves];
-    __shared__ int list[kRowThreads], red_i[kRowWaves];
+    __shared__ double red_d[kLater / 64];
+    __shared__ int list[kChunk], red_i[kLater / 64];
     __shared__ float floor_s;
-    for (int first = 0; first < rows; first += kRowThreads) {
+    for (int first = 0; first < rows; first += kChunk) {
         __syncthreads();
         const int n = open_rows(open, first, rows, list, red_i);
         const int cuts = open_cuts(n, most), len = ((a.vocab + cuts - 1) / cuts + 3) & ~3;
@@ -533,7 +545,7 @@ draw_second(Draw a, int rows, const RowState* __restrict__ state, const int* __r
             const RowState w = state[b];
             float s;
             int tok;
-            const double before = draw_before<UNIT_T>(a, b, row, lo, min(a.vocab, lo + len), w, &floor_s, best, red_d, s, tok);
+            const double before = draw_before<kLater, UNIT_T>(a, b, row, lo, min(a.vocab, lo + len), w, &floor_s, best, red_d, s, tok);
             if (threadIdx.x == 0) {
                 second[(int64_t)b * most + item % cuts] = SecondPart{before, s, tok};
                 cuts_of[b] = cuts;  // (the same from every stretch)
@@ -545,7 +557,7 @@ draw_second(Draw a, int rows, const RowState* __restrict__ state, const int* __r
 // Whether the mass before (l, i) is below top_p of the row's, in float64 throughout.
 DASH_DEV bool kept_exactly(const Draw& a, const float* row, float l0, int i0, float top, double* red) {
     double before = 0.0, all = 0.0;
-    walk_row<2, false>(row, 0, a.vocab, [&](const f32x4_t& l, int i) {
+    walk_row<2, false, kLater>(row, 0, a.vocab, [&](const f32x4_t& l, int i) {
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
             if (!(fabsf(l[j]) < INFINITY)) continue;
@@ -554,20 +566,20 @@ DASH_DEV bool kept_exactly(const Draw& a, const float* row, float l0, int i0, fl
             if (l[j] > l0 || (l[j] == l0 && i + j < i0)) before += e;
         }
     });
-    before = block_sum_d(before, red);
-    all = block_sum_d(all, red);
+    before = block_sum_d<kLater>(before, red);
+    all = block_sum_d<kLater>(all, red);
     return before < a.top_p * all;
 }
 
 template <bool UNIT_T>
-__global__ void __launch_bounds__(kRowThreads)
+__global__ void __launch_bounds__(kLater)
 draw_last(Draw a, int rows, const RowState* __restrict__ state, const int* __restrict__ open, int most,
           const SecondPart* __restrict__ second, const int* __restrict__ cuts_of) {
     __shared__ BestShared best;
-    __shared__ double red_d[kRowWaves];
-    __shared__ int list[kRowThreads], red_i[kRowWaves];
+    __shared__ double red_d[kLater / 64];
+    __shared__ int list[kChunk], red_i[kLater / 64];
     __shared__ float floor_s;
-    for (int first = 0; first < rows; first += kRowThreads) {
+    for (int first = 0; first < rows; first += kChunk) {
         __syncthreads();
         const int n = open_rows(open, first, rows, list, red_i);
         for (int item = blockIdx.x; item < n; item += gridDim.x) {
@@ -605,7 +617,7 @@ draw_last(Draw a, int rows, const RowState* __restrict__ state, const int* __res
                 if (a.top_p >= 1.0 || kept_by_own_mass(a, w.l, w.top, w.z)) break;
                 if (w.bin_ref == w.bin_ref && bin_of(__builtin_amdgcn_exp2f((w.l - w.bin_ref) * a.scale)) >= w.sure) break;
                 w.unsure = 1;
-                before = draw_before<UNIT_T>(a, b, row, 0, a.vocab, w, &floor_s, best, red_d, s, next);
+                before = draw_before<kLater, UNIT_T>(a, b, row, 0, a.vocab, w, &floor_s, best, red_d, s, next);
             }
             if (threadIdx.x == 0) write_draw(a, b, w.tok, ((double)w.l - (double)w.top) / (double)a.temperature - log(w.z));
         }
@@ -687,8 +699,8 @@ hipError_t launch_sample_truncated(const float* logits, int64_t ld, int rows, in
         else if (min_p > 0.0) first(std::false_type{}, std::true_type{});
         else first(std::false_type{}, std::false_type{});
         if (top_p < 1.0 || min_p > 0.0) {  // (otherwise every row has ended)
-            draw_second<U><<<kDrawTarget, kRowThreads, 0, st>>>(a, rows, state, open, p.most, second, cuts_of);
-            draw_last<U><<<std::min(rows, kDrawTarget), kRowThreads, 0, st>>>(a, rows, state, open, p.most, second, cuts_of);
+            draw_second<U><<<kDrawTarget, kLater, 0, st>>>(a, rows, state, open, p.most, second, cuts_of);
+            draw_last<U><<<std::min(rows, kDrawTarget / 2), kLater, 0, st>>>(a, rows, state, open, p.most, second, cuts_of);
         }
         return hipGetLastError();
     };
