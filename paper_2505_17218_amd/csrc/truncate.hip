@@ -22,7 +22,8 @@
 //                tokens before it that the histogram does not rule out; each row cut into stretches,
 //                so that few rows still fill the GPU.
 //   draw_last    joins these; the second winner is nearly always settled by the histogram, too.  What is
-//                left takes further passes of one work-group.
+//                left takes another round of both, if there are many rows, and then further passes
+//                of one work-group.
 // Few rows are cut into stretches in the first pass as well, joined by draw_join.
 // Masses are float32 exponentials first; only where they are within kMassTol of the border, the sums
 // are repeated in float64, so the decision is that of float64 sums.
@@ -235,7 +236,8 @@ DASH_DEV void settle(const Draw& a, int b, const float* row, int tok, float top,
         }
     }
     if (threadIdx.x != 0) return;
-    open[b] = !done;
+    open[2 * b] = !done;  // for the first round of the later passes, and the second
+    open[2 * b + 1] = 0;
     if (!done) state[b] = r;
     else if (tok == kNone) write_draw(a, b, -1, 0.0);
     else write_draw(a, b, tok, ((double)r.l - (double)top) / (double)a.temperature - log(z));
@@ -342,13 +344,13 @@ draw_first(Draw a, RowSplit cut, FirstPart* __restrict__ part, uint32_t* __restr
     const int copy = threadIdx.x & (kCopies - 1);
     float ref = -FLT_MAX, bins_at = NAN, top = -INFINITY;
     double z = 0.0;
-    walk_row<4, true, false>(
+    walk_row<2, true, false>(
         row, SPLIT ? n * cut.len : 0, SPLIT ? min(a.vocab, (n + 1) * cut.len) : a.vocab,
-        [&](const f32x4_t (&buf)[4], int) {
+        [&](const f32x4_t (&buf)[2], int) {
             // The reference of the sums and of the bins: the largest of a sample of the row.
             float m = -INFINITY;
 #pragma unroll
-            for (int d = 0; d < 4; ++d)
+            for (int d = 0; d < 2; ++d)
 #pragma unroll
                 for (int j = 0; j < 4; ++j) m = fmaxf(m, buf[d][j] < INFINITY ? buf[d][j] : -INFINITY);
             m = block_max_f(m, red_f);
@@ -510,13 +512,13 @@ DASH_DEV double draw_before(const Draw& a, int b, const float* row, int lo, int 
 // The later passes have work-groups of kLater threads: with 1024 the last one needed more registers than
 // there are, and a launch with scratch memory took 20 us with nothing to do.  They take rows by chunks.
 constexpr int kLater = 512, kChunk = 1024;
-// The rows that are open among rows [first, first + kChunk), in order; returns their number.
-DASH_DEV int open_rows(const int* open, int first, int rows, int* list, int* red) {
+// The rows that are open in a round (0 or 1) among rows [first, first + kChunk), in order; returns their number.
+DASH_DEV int open_rows(const int* open, int round, int first, int rows, int* list, int* red) {
     constexpr int kOwn = kChunk / kLater;
     const int r = first + kOwn * (int)threadIdx.x;
     int mine[kOwn], sum = 0, total;
 #pragma unroll
-    for (int o = 0; o < kOwn; ++o) sum += mine[o] = r + o < rows && open[r + o];
+    for (int o = 0; o < kOwn; ++o) sum += mine[o] = r + o < rows && open[2 * (r + o) + round];
     int at = block_scan<kLater>(sum, red, total) - sum;
 #pragma unroll
     for (int o = 0; o < kOwn; ++o)
@@ -529,15 +531,15 @@ DASH_DEV int open_cuts(int n, int most) { return max(1, min(most, (int)gridDim.x
 
 template <bool UNIT_T>
 __global__ void __launch_bounds__(kLater)
-draw_second(Draw a, int rows, const RowState* __restrict__ state, const int* __restrict__ open, int most,
-            SecondPart* __restrict__ second, int* __restrict__ cuts_of) {
+draw_second(Draw a, int rows, const RowState* __restrict__ state, const int* __restrict__ open, int round,
+            int most, SecondPart* __restrict__ second, int* __restrict__ cuts_of) {
     __shared__ BestShared best;
     __shared__ double red_d[kLater / 64];
     __shared__ int list[kChunk], red_i[kLater / 64];
     __shared__ float floor_s;
     for (int first = 0; first < rows; first += kChunk) {
         __syncthreads();
-        const int n = open_rows(open, first, rows, list, red_i);
+        const int n = open_rows(open, round, first, rows, list, red_i);
         const int cuts = open_cuts(n, most), len = ((a.vocab + cuts - 1) / cuts + 3) & ~3;
         for (int item = blockIdx.x; item < n * cuts; item += gridDim.x) {
             const int b = list[item / cuts], lo = min(a.vocab, item % cuts * len);
@@ -571,9 +573,10 @@ DASH_DEV bool kept_exactly(const Draw& a, const float* row, float l0, int i0, fl
     return before < a.top_p * all;
 }
 
-template <bool UNIT_T>
+// LAST: rows that are still in doubt take further passes here; otherwise they stay open for another round.
+template <bool UNIT_T, bool LAST>
 __global__ void __launch_bounds__(kLater)
-draw_last(Draw a, int rows, const RowState* __restrict__ state, const int* __restrict__ open, int most,
+draw_last(Draw a, int rows, RowState* __restrict__ state, int* __restrict__ open, int round, int most,
           const SecondPart* __restrict__ second, const int* __restrict__ cuts_of) {
     __shared__ BestShared best;
     __shared__ double red_d[kLater / 64];
@@ -581,7 +584,7 @@ draw_last(Draw a, int rows, const RowState* __restrict__ state, const int* __res
     __shared__ float floor_s;
     for (int first = 0; first < rows; first += kChunk) {
         __syncthreads();
-        const int n = open_rows(open, first, rows, list, red_i);
+        const int n = open_rows(open, round, first, rows, list, red_i);
         for (int item = blockIdx.x; item < n; item += gridDim.x) {
             const int b = list[item], cuts = cuts_of[b], lane = threadIdx.x & 63;
             const float* row = a.logits + (int64_t)(a.row_of ? a.row_of[b] : b) * a.ld;
@@ -605,6 +608,7 @@ draw_last(Draw a, int rows, const RowState* __restrict__ state, const int* __res
                     next = oi;
                 }
             }
+            bool ended = true;
             for (;;) {
                 bool kept = false;
                 if (w.unsure) {
@@ -617,9 +621,19 @@ draw_last(Draw a, int rows, const RowState* __restrict__ state, const int* __res
                 if (a.top_p >= 1.0 || kept_by_own_mass(a, w.l, w.top, w.z)) break;
                 if (w.bin_ref == w.bin_ref && bin_of(__builtin_amdgcn_exp2f((w.l - w.bin_ref) * a.scale)) >= w.sure) break;
                 w.unsure = 1;
+                if constexpr (!LAST) {
+                    ended = false;
+                    break;
+                }
                 before = draw_before<kLater, UNIT_T>(a, b, row, 0, a.vocab, w, &floor_s, best, red_d, s, next);
             }
-            if (threadIdx.x == 0) write_draw(a, b, w.tok, ((double)w.l - (double)w.top) / (double)a.temperature - log(w.z));
+            if (threadIdx.x != 0) continue;
+            if (!ended) {
+                state[b] = w;
+                open[2 * b + 1] = 1;
+            } else {
+                write_draw(a, b, w.tok, ((double)w.l - (double)w.top) / (double)a.temperature - log(w.z));
+            }
         }
     }
 }
@@ -646,7 +660,7 @@ DrawPlan draw_plan(int rows, int vocab) {
     p.parts = take(stretches * sizeof(FirstPart));
     p.states = take(n * sizeof(RowState));
     p.seconds = take((size_t)n * p.most * sizeof(SecondPart));
-    p.opens = take(2 * (size_t)n * sizeof(int));
+    p.opens = take(3 * (size_t)n * sizeof(int));
     p.bytes = at;
     return p;
 }
@@ -683,7 +697,7 @@ hipError_t launch_sample_truncated(const float* logits, int64_t ld, int rows, in
         RowState* state = (RowState*)(at + p.states);
         SecondPart* second = (SecondPart*)(at + p.seconds);
         int* open = (int*)(at + p.opens);
-        int* cuts_of = open + rows;
+        int* cuts_of = open + 2 * (size_t)rows;
         auto first = [&](auto hist, auto minp) {
             constexpr bool H = decltype(hist)::value, M = decltype(minp)::value;
             if (p.first.n == 1) {
@@ -699,8 +713,16 @@ hipError_t launch_sample_truncated(const float* logits, int64_t ld, int rows, in
         else if (min_p > 0.0) first(std::false_type{}, std::true_type{});
         else first(std::false_type{}, std::false_type{});
         if (top_p < 1.0 || min_p > 0.0) {  // (otherwise every row has ended)
-            draw_second<U><<<kDrawTarget, kLater, 0, st>>>(a, rows, state, open, p.most, second, cuts_of);
-            draw_last<U><<<std::min(rows, kDrawTarget / 2), kLater, 0, st>>>(a, rows, state, open, p.most, second, cuts_of);
+            const int grid = std::min(rows, kDrawTarget / 2);
+            // Of many rows one is likely to need a third pass, which takes one work-group as long as all the rest:
+            // a second round costs 9 us and leaves that to few calls.
+            const bool again = rows >= 256;
+            draw_second<U><<<kDrawTarget, kLater, 0, st>>>(a, rows, state, open, 0, p.most, second, cuts_of);
+            if (again) {
+                draw_last<U, false><<<grid, kLater, 0, st>>>(a, rows, state, open, 0, p.most, second, cuts_of);
+                draw_second<U><<<kDrawTarget, kLater, 0, st>>>(a, rows, state, open, 1, p.most, second, cuts_of);
+            }
+            draw_last<U, true><<<grid, kLater, 0, st>>>(a, rows, state, open, again, p.most, second, cuts_of);
         }
         return hipGetLastError();
     };
