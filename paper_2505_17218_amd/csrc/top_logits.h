@@ -19,6 +19,7 @@
 #pragma once
 
 #include <algorithm>
+#include <type_traits>
 
 #include "row_walk.h"
 
@@ -119,9 +120,16 @@ DASH_DEV W top_bound(BoundShared<NT>& sh, const W (&e)[PER], int per, int k, int
 
 // ---- the second launch -----------------------------------------------------------------------------
 
-// A work-group of NT threads holds NT PER words: 256 x 16 for K up to 256, where several rows share a
-// CU and a barrier is of four waves; 1024 x 8 above.
+// A work-group of NT threads holds NT PER words.  It has as many threads as there may be results, but not
+// fewer than 256: small ones share a CU, and their barriers are of few waves (333 rows and K = 500: 44 us
+// with 1024 threads, whose registers leave one to a CU).
 constexpr int kTopSmall = 256;
+template <class F>
+void top_join_variant(int k, F&& join) {
+    if (k <= kTopSmall) join(std::integral_constant<int, 256>{}, std::integral_constant<int, 16>{});
+    else if (k <= 512) join(std::integral_constant<int, 512>{}, std::integral_constant<int, 16>{});
+    else join(std::integral_constant<int, 1024>{}, std::integral_constant<int, 8>{});
+}
 template <int NT, int PER>
 struct TopShared {
     uint64_t c[NT * PER];

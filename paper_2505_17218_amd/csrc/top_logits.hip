@@ -7,7 +7,7 @@ namespace dash {
 
 namespace {
 
-constexpr int kTopTarget = 512, kTopStretch = 4096, kTopRoom = 16384;
+constexpr int kTopTarget = 1024, kTopStretch = 8192, kTopRoom = 16384;
 
 __global__ void __launch_bounds__(kRowThreads, 8)
 top_part_k(const float* __restrict__ logits, int64_t ld, int vocab, const int32_t* __restrict__ row_of, int k,
@@ -136,10 +136,11 @@ hipError_t launch_top_logits(const float* logits, int64_t ld, int rows, int voca
     if (hipError_t e = launch_top_parts(logits, ld, rows, vocab, nullptr, k, temperature, top_plan(rows, vocab, k), ws, p, st))
         return e;
     const float scale = exp2_scale(temperature);
-    if (k <= kTopSmall)
-        top_logits_k<256, 16><<<rows, 256, 0, st>>>(logits, ld, vocab, k, (double)temperature, scale, p, values, indices, rest);
-    else
-        top_logits_k<1024, 8><<<rows, 1024, 0, st>>>(logits, ld, vocab, k, (double)temperature, scale, p, values, indices, rest);
+    auto join = [&](auto threads, auto per) {
+        constexpr int NT = decltype(threads)::value, PER = decltype(per)::value;
+        top_logits_k<NT, PER><<<rows, NT, 0, st>>>(logits, ld, vocab, k, (double)temperature, scale, p, values, indices, rest);
+    };
+    top_join_variant(k, join);
     return hipGetLastError();
 }
 

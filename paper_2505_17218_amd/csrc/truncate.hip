@@ -686,8 +686,10 @@ hipError_t launch_sample_truncated(const float* logits, int64_t ld, int rows, in
             if (hipError_t e = launch_top_parts(logits, ld, rows, vocab, row_of, top_k, temperature,
                                                 top_plan(rows, vocab, top_k), ws, parts, st))
                 return e;
-            if (top_k <= kTopSmall) draw_top_k<U, 256, 16><<<rows, 256, 0, st>>>(a, parts);
-            else draw_top_k<U, 1024, 8><<<rows, 1024, 0, st>>>(a, parts);
+            top_join_variant(top_k, [&](auto threads, auto per) {
+                constexpr int NT = decltype(threads)::value, PER = decltype(per)::value;
+                draw_top_k<U, NT, PER><<<rows, NT, 0, st>>>(a, parts);
+            });
             return hipGetLastError();
         }
         const DrawPlan p = draw_plan(rows, vocab);

@@ -160,21 +160,23 @@ def sample(logits: torch.Tensor, seq_uid: torch.Tensor, step: torch.Tensor, temp
     return toks, lps
 
 
-def _check_rows(logits: torch.Tensor, **rows) -> None:
-    """float32 logits [rows, vocab] on a GPU with unit column stride, and tensors of one value (or k) per row beside
-    them: name=(tensor or None, dtype, shape).  The kernels run on the current device and stream."""
+def _check_rows(logits: torch.Tensor) -> int:
+    """float32 logits [rows, vocab] with unit column stride on the current GPU, where the kernels run; its index."""
     if logits.dim() != 2 or logits.dtype != torch.float32 or not logits.is_cuda:
         raise ValueError("logits must be a float32 [rows, vocab] tensor on the GPU")
-    if logits.shape[1] < 1 or (logits.shape[1] > 1 and logits.stride(1) != 1) or \
-            (logits.shape[0] > 1 and logits.stride(0) < logits.shape[1]):
+    rows, V = logits.shape
+    if V < 1 or (V > 1 and logits.stride(1) != 1) or (rows > 1 and logits.stride(0) < V):
         raise ValueError("logits need unit column stride and rows that do not overlap")
-    if logits.device.index != torch.cuda.current_device():
-        raise ValueError(f"logits are on {logits.device}, the current device is cuda:{torch.cuda.current_device()}")
-    for name, (t, dtype, shape) in rows.items():
-        if t is None:
-            continue
-        if t.device != logits.device or t.dtype != dtype or tuple(t.shape) != shape or not t.is_contiguous():
-            raise ValueError(f"{name} must be a contiguous {dtype} tensor of shape {shape} on {logits.device}")
+    device = logits.get_device()
+    if device != torch.cuda.current_device():
+        raise ValueError(f"logits are on cuda:{device}, the current device is cuda:{torch.cuda.current_device()}")
+    return device
+
+
+def _check_beside(device: int, name: str, t: torch.Tensor | None, dtype: torch.dtype, shape: tuple) -> None:
+    """A contiguous tensor beside the logits, or None."""
+    if t is not None and (t.dtype != dtype or t.shape != shape or t.get_device() != device or not t.is_contiguous()):
+        raise ValueError(f"{name} must be a contiguous {dtype} tensor of shape {shape} on cuda:{device}")
 
 
 def _ld(t: torch.Tensor) -> int:
@@ -196,8 +198,11 @@ def sample_truncated(logits: torch.Tensor, seq_uid: torch.Tensor, step: torch.Te
     seq_uid.  top_k 0, top_p 1 and min_p 0 each keep every token.  row_of int32 [n]: the logits row of each draw,
     which must lie in [0, rows) (it is not checked); status int32 [1] (bits OR-ed in)."""
     n = seq_uid.numel()
-    _check_rows(logits, seq_uid=(seq_uid, torch.int32, (n,)), step=(step, torch.int32, (n,)),
-                row_of=(row_of, torch.int32, (n,)), status=(status, torch.int32, (1,)))
+    device = _check_rows(logits)
+    _check_beside(device, "seq_uid", seq_uid, torch.int32, (n,))
+    _check_beside(device, "step", step, torch.int32, (n,))
+    _check_beside(device, "row_of", row_of, torch.int32, (n,))
+    _check_beside(device, "status", status, torch.int32, (1,))
     if row_of is None and n > logits.shape[0]:
         raise ValueError(f"{n} draws from {logits.shape[0]} rows of logits")
     toks = torch.empty(n, dtype=torch.int32, device=logits.device)
@@ -226,13 +231,16 @@ def top_logits(logits: torch.Tensor, k: int, temperature: float = 1.0):
 
 
 def _check_distill(logits, values, indices, rest, norm=None, weight=None):
+    if logits.dim() != 2 or values.dim() != 2:
+        raise ValueError("logits must be [rows, vocab] and the teacher's values [rows, k]")
     rows = logits.shape[0]
-    if values.dim() != 2:
-        raise ValueError("the teacher's values must be [rows, k]")
     k = values.shape[1]
-    _check_rows(logits, values=(values, torch.float32, (rows, k)), indices=(indices, torch.int32, (rows, k)),
-                rest=(rest, torch.float32, (rows,)), norm=(norm, torch.float32, (rows, 4)),
-                weight=(weight, torch.float32, (rows,)))
+    device = _check_rows(logits)
+    _check_beside(device, "values", values, torch.float32, (rows, k))
+    _check_beside(device, "indices", indices, torch.int32, (rows, k))
+    _check_beside(device, "rest", rest, torch.float32, (rows,))
+    _check_beside(device, "norm", norm, torch.float32, (rows, 4))
+    _check_beside(device, "weight", weight, torch.float32, (rows,))
     return rows, logits.shape[1], k
 
 
