@@ -120,7 +120,7 @@ DASH_DEV ExpSum sum_others(const DistillArgs& a, const float* row, const Teacher
     if (threadIdx.x == 0) twice = 0;
     for (int base = lo; base < hi; base += kStretch) {
         const int end = min(hi, base + kStretch);
-        walk_row<4, false, false, NT>(
+        walk_row<4, false, true, NT>(
             row, base, end,
             [&](const f32x4_t (&)[4], int) { mark_tokens(mark, twice, t, base, end - base); },  // (the first loads are under way)
             [&](f32x4_t l, int i) {
@@ -187,7 +187,7 @@ DASH_DEV void store4(G* p, const float (&v)[4], int n);
 template <>
 DASH_DEV void store4<float>(float* p, const float (&v)[4], int n) {
     if (n >= 4) {
-        *reinterpret_cast<f32x4u_t*>(p) = f32x4_t{v[0], v[1], v[2], v[3]};
+        __builtin_nontemporal_store(f32x4_t{v[0], v[1], v[2], v[3]}, reinterpret_cast<f32x4u_t*>(p));
     } else {
         for (int j = 0; j < n; ++j) p[j] = v[j];
     }
@@ -197,7 +197,7 @@ DASH_DEV void store4<bf16_t>(bf16_t* p, const float (&v)[4], int n) {
     typedef uint32_t u32x2_t __attribute__((ext_vector_type(2)));
     typedef u32x2_t u32x2u_t __attribute__((aligned(2)));
     if (n >= 4) {
-        *reinterpret_cast<u32x2u_t*>(p) = u32x2_t{f2bf2(v[0], v[1]), f2bf2(v[2], v[3])};
+        __builtin_nontemporal_store(u32x2_t{f2bf2(v[0], v[1]), f2bf2(v[2], v[3])}, reinterpret_cast<u32x2u_t*>(p));
     } else {
         for (int j = 0; j < n; ++j) p[j] = f2bf(v[j]);
     }
@@ -249,7 +249,7 @@ DASH_DEV void row_grad(const DistillArgs& a, const float* row, G* grad, int lo, 
     float g[Teacher<NT>::kOwn];
     const GradTerms q = grad_terms(a, t, s, n, w, lo, hi, g);
     __syncthreads();
-    walk_row<4, false, NT>(row, lo, hi, [&](const f32x4_t& l, int i) {
+    walk_row<4, true, NT>(row, lo, hi, [&](const f32x4_t& l, int i) {
         float v[4];
         grad4(a, q, l, v);
         store4(grad + i, v, hi - i);
@@ -387,7 +387,7 @@ distill_loss_grad_k(DistillArgs a) {
     f32x4_t in[kInRegs];
 #pragma unroll
     for (int d = 0; d < kInRegs; ++d)
-        if (d < whole) in[d] = load_row4<false>(row, at + d * kTile);
+        if (d < whole) in[d] = load_row4<true>(row, at + d * kTile);
     Teacher<kWide> t;
     float s[t.kOwn];
     load_tokens(a, r, t);
