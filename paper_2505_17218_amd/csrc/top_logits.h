@@ -150,9 +150,43 @@ struct TopState {
     ExpSum rest;       // the thread's share of the entries that were turned away
 };
 
+// The words that each(f) calls f with, all threads' together, join the rest; out is the largest key among
+// the thread's.  Integer terms relative to the largest of all: their sum does not depend on the order
+// of the words, which varies with the order in which waves appended them.  (sh.evict_z and
+// sh.evict_ref are 0, set a barrier ago.)
+template <int NT, int PER, class EACH>
+DASH_DEV void top_turn_away(TopShared<NT, PER>& sh, TopState& st, unsigned out, float scale, EACH&& each) {
+    if (__any(out != 0)) {
+#pragma unroll
+        for (int o = 32; o >= 1; o >>= 1) out = max(out, (unsigned)__shfl_xor((int)out, o, 64));
+        if ((threadIdx.x & 63) == 0) atomicMax(&sh.evict_ref, out);
+    }
+    __syncthreads();
+    const unsigned top = sh.evict_ref;
+    if (!top) return;
+    const float ref = top_value(top);
+    uint64_t z = 0;
+    each([&](uint64_t w) { z += (uint64_t)(__builtin_amdgcn_exp2f((word_value(w) - ref) * scale) * kEvictOne); });
+    if (__any(z != 0)) {
+#pragma unroll
+        for (int o = 32; o >= 1; o >>= 1) z += (uint64_t)__shfl_xor((long long)z, o, 64);
+        if ((threadIdx.x & 63) == 0) atomicAdd((unsigned long long*)&sh.evict_z, (unsigned long long)z);
+    }
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        const double zd = (double)sh.evict_z / (double)kEvictOne;
+        if (ref > st.rest.ref) {
+            st.rest.z = st.rest.z * exp2((double)(st.rest.ref - ref) * (double)scale) + zd;
+            st.rest.ref = ref;
+        } else {
+            st.rest.z += zd * exp2((double)(ref - st.rest.ref) * (double)scale);
+        }
+    }
+}
+
 // Of n words in the threads' registers (word r NT + thread is e[r]; 0: none) those at or above a bound
-// that leaves k .. k + slack of them (all, if n is no more) go to LDS, the others join the rest.
-template <int NT, int PER>
+// that leaves k .. k + slack of them (all, if n is no more) go to LDS, the others (SUM) join the rest.
+template <bool SUM, int NT, int PER>
 DASH_DEV void top_keep(TopShared<NT, PER>& sh, TopState& st, const uint64_t (&e)[PER], int n, int k, int slack, float scale) {
     const int per = (n + NT - 1) / NT;
     int count = n;
@@ -176,46 +210,21 @@ DASH_DEV void top_keep(TopShared<NT, PER>& sh, TopState& st, const uint64_t (&e)
         }
         if (e[r] && e[r] < b) out = max(out, (unsigned)(e[r] >> 32));
     }
-    if (__any(out != 0)) {
+    if constexpr (SUM)
+        top_turn_away(sh, st, out, scale, [&](auto&& f) {
 #pragma unroll
-        for (int o = 32; o >= 1; o >>= 1) out = max(out, (unsigned)__shfl_xor((int)out, o, 64));
-        if ((threadIdx.x & 63) == 0) atomicMax(&sh.evict_ref, out);
-    }
-    __syncthreads();
-    // Integer terms relative to the largest: their sum does not depend on the order of the words,
-    // which varies with the order in which waves appended them.
-    const unsigned top = sh.evict_ref;
-    if (top) {
-        const float ref = top_value(top);
-        uint64_t z = 0;
-#pragma unroll
-        for (int r = 0; r < PER; ++r) {
-            if (r >= per) break;
-            if (e[r] && e[r] < b) z += (uint64_t)(__builtin_amdgcn_exp2f((word_value(e[r]) - ref) * scale) * kEvictOne);
-        }
-        if (__any(z != 0)) {
-#pragma unroll
-            for (int o = 32; o >= 1; o >>= 1) z += (uint64_t)__shfl_xor((long long)z, o, 64);
-            if ((threadIdx.x & 63) == 0) atomicAdd((unsigned long long*)&sh.evict_z, (unsigned long long)z);
-        }
-        __syncthreads();
-        if (threadIdx.x == 0) {
-            const double zd = (double)sh.evict_z / (double)kEvictOne;
-            if (ref > st.rest.ref) {
-                st.rest.z = st.rest.z * exp2((double)(st.rest.ref - ref) * (double)scale) + zd;
-                st.rest.ref = ref;
-            } else {
-                st.rest.z += zd * exp2((double)(ref - st.rest.ref) * (double)scale);
+            for (int r = 0; r < PER; ++r) {
+                if (r >= per) break;
+                if (e[r] && e[r] < b) f(e[r]);
             }
-        }
-    }
+        });
     if (threadIdx.x == 0) sh.count = count;
     st.n = count;
-    st.low = b;
+    st.low = max(st.low, b);  // (no cut was needed: b is the lowest word)
 }
 
 // Cuts the words in LDS to k .. k + slack.
-template <int NT, int PER>
+template <bool SUM, int NT, int PER>
 DASH_DEV void top_cut(TopShared<NT, PER>& sh, TopState& st, int k, int slack, float scale) {
     uint64_t e[PER];
 #pragma unroll
@@ -223,7 +232,7 @@ DASH_DEV void top_cut(TopShared<NT, PER>& sh, TopState& st, int k, int slack, fl
         const int i = r * NT + (int)threadIdx.x;
         e[r] = i < st.n ? sh.c[i] : 0;
     }
-    top_keep(sh, st, e, st.n, k, slack, scale);
+    top_keep<SUM>(sh, st, e, st.n, k, slack, scale);
     __syncthreads();
 }
 
@@ -284,49 +293,60 @@ DASH_DEV void top_gather(TopShared<NT, PER>& sh, TopState& st, const TopParts& p
             const int i = r * NT + (int)threadIdx.x;
             e[r] = i < total ? word(i) : 0;
         }
-        top_keep(sh, st, e, total, k, total > p ? p - k : total, scale);
+        top_keep<true>(sh, st, e, total, k, total > p ? p - k : total, scale);
         __syncthreads();
         return;
     }
     const int slack = (k >> 2) + 32;
-    auto count = [&] {  // after at most kTile appends: room for as many again
+    auto count = [&](auto sum) {  // after at most kTile appends: room for as many again
         __syncthreads();
         st.n = sh.count;
         __syncthreads();
-        if (st.n > kCap - kTile) top_cut(sh, st, k, slack, scale);
+        if (st.n > kCap - kTile) top_cut<decltype(sum)::value>(sh, st, k, slack, scale);
     };
     if (fits) {
+        // Which words share a piece depends on the order of the lists, so none joins the rest before
+        // the k largest are known.
         for (int from = 0; from < total; from += kTile) {
 #pragma unroll 1
             for (int i = from + (int)threadIdx.x; i - lane < min(total, from + kTile); i += NT) {
                 const uint64_t w = i < total ? word(i) : 0;
                 top_append(sh, w >= max(st.low, (uint64_t)1), w);
-                if (w && w < st.low) {
-                    const float l = word_value(w);
-                    exp_push1(st.rest, l, scale);
-                }
             }
-            count();
+            count(std::false_type{});
         }
-    } else {
-        st = TopState{};
-#pragma unroll 1
-        for (int at = 0; at < vocab; at += kTile) {
-            walk_row<1, true, NT>(row, at, min(vocab, at + kTile), [&](f32x4_t l, int i) {
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    const bool entry = fabsf(l[j]) < INFINITY;
-                    const uint64_t w = entry ? top_word(l[j], i + j) : 0;
-                    const bool in = entry && w >= st.low;
-                    top_append(sh, in, w);
-                    if (in || !entry) l[j] = -INFINITY;
-                }
-                exp_push4<false>(st.rest, l, max4(l), scale);
-            });
-            count();
+        top_cut<false>(sh, st, k, 0, scale);
+        unsigned out = 0;
+        for (int i = threadIdx.x; i < total; i += NT) {
+            const uint64_t w = word(i);
+            if (w < st.low) out = max(out, (unsigned)(w >> 32));
         }
+        top_turn_away(sh, st, out, scale, [&](auto&& f) {
+            for (int i = threadIdx.x; i < total; i += NT) {
+                const uint64_t w = word(i);
+                if (w < st.low) f(w);
+            }
+        });
+        __syncthreads();
+        return;
     }
-    if (st.n > p) top_cut(sh, st, k, p - k, scale);
+    st = TopState{};
+#pragma unroll 1
+    for (int at = 0; at < vocab; at += kTile) {
+        walk_row<1, true, NT>(row, at, min(vocab, at + kTile), [&](f32x4_t l, int i) {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const bool entry = fabsf(l[j]) < INFINITY;
+                const uint64_t w = entry ? top_word(l[j], i + j) : 0;
+                const bool in = entry && w >= st.low;
+                top_append(sh, in, w);
+                if (in || !entry) l[j] = -INFINITY;
+            }
+            exp_push4<false>(st.rest, l, max4(l), scale);
+        });
+        count(std::true_type{});
+    }
+    if (st.n > p) top_cut<true>(sh, st, k, p - k, scale);
 }
 
 // Words that a row's selection leaves at most: sorting pads to it.

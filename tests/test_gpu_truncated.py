@@ -149,6 +149,26 @@ def test_sample_large(rows, V, top_k, top_p, min_p):
     _check_sample(_rows("peak", rows, V, 6), 0.8, top_k, top_p, min_p)
 
 
+@pytest.mark.parametrize("top_k, top_p, min_p", [(50, 0.9, 0.0), (700, 0.99, 0.0), (0, 0.95, 0.0), (0, 1.0, 0.05), (0, 0.5, 0.0),
+                                                 (0, 0.7, 0.01), (0, 1.0, 0.0)])
+def test_sample_many_rows(top_k, top_p, min_p):
+    """Enough rows that none is cut into stretches."""
+    require_gpu()
+    row_of = np.arange(600) % 97
+    l = _rows("normal", 97, 9001, 18)
+    l[50:] = _rows("peak", 47, 9001, 18)
+    l[7] = -np.inf
+    _check_sample(l, 0.9, top_k, top_p, min_p, row_of=row_of)
+
+
+@pytest.mark.parametrize("rows", [3, 260])
+@pytest.mark.parametrize("top_p, min_p", [(0.95, 0.0), (0.4, 0.0), (1.0, 0.1)])
+def test_sample_long_rows(rows, top_p, min_p):
+    """Rows of more than 2^18 tokens."""
+    require_gpu()
+    _check_sample(_rows("normal", 3, (1 << 18) + 77, 19), 1.0, 0, top_p, min_p, row_of=np.arange(rows) % 3)
+
+
 def test_small_and_large_temperatures():
     require_gpu()
     l = _rows("normal", 4, 3001, 8)
@@ -232,6 +252,21 @@ def test_equal_calls_give_equal_bits():
     first = engine.top_logits(l, 200, 0.7), engine.sample_truncated(l, uid, uid, 0.7, 1, 0, 0.9)
     for _ in range(5):
         again = engine.top_logits(l, 200, 0.7), engine.sample_truncated(l, uid, uid, 0.7, 1, 0, 0.9)
+        for a, b in zip(first, again):
+            assert all(torch.equal(x, y) for x, y in zip(a, b))
+
+
+@pytest.mark.parametrize("kind, V, k", [("peak", 151936, 1024), ("up", 151936, 900), ("normal", 50257, 1000)])
+def test_equal_calls_give_equal_bits_for_many_entries(kind, V, k):
+    """Lists of candidates too long to be cut at once, in an order that differs between calls."""
+    require_gpu()
+    l = torch.from_numpy(_rows(kind, 4, V, 20)).cuda().repeat(10, 1)
+    uid = dev_i32(np.arange(40))
+    first = engine.top_logits(l, k, 0.7), engine.sample_truncated(l, uid, uid, 0.7, 1, k, 0.9)
+    for t in first[0]:
+        assert torch.equal(t[:4], t[36:])
+    for _ in range(5):
+        again = engine.top_logits(l, k, 0.7), engine.sample_truncated(l, uid, uid, 0.7, 1, k, 0.9)
         for a, b in zip(first, again):
             assert all(torch.equal(x, y) for x, y in zip(a, b))
 
