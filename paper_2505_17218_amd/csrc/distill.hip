@@ -295,6 +295,10 @@ distill_loss_k(DistillArgs a) {
     __shared__ MarkShared mark;
     const int64_t r = blockIdx.x;
     const float* row = a.logits + r * a.ld;
+    if (a.weight && a.weight[r] == 0.f) {
+        if (threadIdx.x == 0) a.loss[r] = 0.f;
+        return;
+    }
     Teacher<kWide> t;
     float s[t.kOwn];
     load_tokens(a, r, t);
