@@ -120,16 +120,19 @@ DASH_DEV W top_bound(BoundShared<NT>& sh, const W (&e)[PER], int per, int k, int
 
 // ---- the second launch -----------------------------------------------------------------------------
 
-// A work-group of NT threads holds NT PER words.  It has as many threads as there may be results, but not
-// fewer than 256: small ones share a CU, and their barriers are of few waves (333 rows and K = 500: 44 us
-// with 1024 threads, whose registers leave one to a CU).
+// A work-group of NT threads holds NT PER words, as many as a row's lists have together as a rule
+// (k = 1000 of 151,936 cut piece by piece, 8192 words at a time: 672 us for 2048 rows, 568 whole).  It has as
+// many threads as there may be results, but not fewer than 256: small ones share a CU, and their
+// barriers are of few waves (333 rows and k = 500: 44 us with 1024 threads, 34 with 512).
 constexpr int kTopSmall = 256;
 template <class F>
 void top_join_variant(int k, F&& join) {
-    if (k <= kTopSmall) join(std::integral_constant<int, 256>{}, std::integral_constant<int, 16>{});
+    if (k <= 64) join(std::integral_constant<int, 256>{}, std::integral_constant<int, 8>{});
+    else if (k <= kTopSmall) join(std::integral_constant<int, 256>{}, std::integral_constant<int, 16>{});
     else if (k <= 512) join(std::integral_constant<int, 512>{}, std::integral_constant<int, 16>{});
-    else join(std::integral_constant<int, 1024>{}, std::integral_constant<int, 8>{});
+    else join(std::integral_constant<int, 1024>{}, std::integral_constant<int, 16>{});
 }
+inline int top_cap(int k) { return k <= 64 ? 256 * 8 : k <= kTopSmall ? 256 * 16 : k <= 512 ? 512 * 16 : 1024 * 16; }
 template <int NT, int PER>
 struct TopShared {
     uint64_t c[NT * PER];

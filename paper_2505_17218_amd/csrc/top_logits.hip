@@ -7,7 +7,9 @@ namespace dash {
 
 namespace {
 
-constexpr int kTopTarget = 1024, kTopStretch = 8192, kTopRoom = 16384;
+// Work-groups that run at once (two per CU), shortest stretch, what a stretch costs beside its entries
+// (its bound, its last sums) in entries, longest list.
+constexpr int kTopSlots = 512, kTopStretch = 8192, kTopFixed = 24576, kTopRoom = 16384;
 
 __global__ void __launch_bounds__(kRowThreads, 8)
 top_part_k(const float* __restrict__ logits, int64_t ld, int vocab, const int32_t* __restrict__ row_of, int k,
@@ -60,13 +62,14 @@ top_part_k(const float* __restrict__ logits, int64_t ld, int vocab, const int32_
                 at = __builtin_amdgcn_readfirstlane(at);
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
-                    const int to = at + (int)__builtin_amdgcn_mbcnt_hi((uint32_t)(in[j] >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)in[j], 0u));
-                    if (l[j] > thr) {
-                        if (l[j] < INFINITY && to < plan.room) words[to] = top_word(l[j], i + j);
-                        l[j] = -INFINITY;  // (+inf is no entry either)
-                    }
+                    if (!in[j]) continue;
+                    const uint32_t to = (uint32_t)at + __builtin_amdgcn_mbcnt_hi((uint32_t)(in[j] >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)in[j], 0u));
+                    if (l[j] > thr && l[j] < INFINITY && to < (uint32_t)plan.room)
+                        *reinterpret_cast<uint64_t*>(reinterpret_cast<char*>(words) + to * 8u) = top_word(l[j], i + j);
                     at += __popcll(in[j]);
                 }
+#pragma unroll
+                for (int j = 0; j < 4; ++j) l[j] = l[j] > thr ? -INFINITY : l[j];  // (+inf is no entry either)
             }
             exp_push4<false>(rest, l, max4(l), scale);
         },
@@ -110,7 +113,20 @@ TopPlan top_plan(int rows, int vocab, int k) {
         return r;
     };
     TopPlan p;
-    p.cut = split_row(vocab, std::min({kTopParts, kTopTarget / std::max(rows, 1), vocab / kTopStretch}));
+    // The number of stretches that ends soonest, of those whose lists fit in the second launch's registers: a
+    // stretch lets about k words through however short it is, hence the 2 k each (64 rows and
+    // k = 1000: 59 us, 192 with 16 stretches; and 31 us with 8, 44 with 16 for k = 64).
+    const int most = std::min({kTopParts, 2 * kTopSlots / std::max(rows, 1), vocab / kTopStretch, top_cap(k) / (2 * k)});
+    int best = 1;
+    int64_t least = INT64_MAX;
+    for (int n = 1; n <= most; ++n) {
+        const int64_t rounds = ((int64_t)rows * n + kTopSlots - 1) / kTopSlots, cost = rounds * (vocab / n + kTopFixed);
+        if (cost < least) {
+            least = cost;
+            best = n;
+        }
+    }
+    p.cut = split_row(vocab, best);
     p.room = room(p.cut.len);
     return p;
 }
