@@ -341,7 +341,8 @@ int dash_sample(const float* d_logits, int64_t ld, int32_t n_rows, int32_t vocab
  * than 2^21 rows.  d_ws: dash_sample_truncated_workspace_bytes(n_rows, vocab, top_k)
  * bytes, 256-byte aligned (as every workspace here; may be NULL where that is 0), of which
  * nothing has to be cleared or kept; calls that may overlap in time, and graphs that may
- * be replayed at the same time, need one each.  DASH_ECAPACITY if it is too small.
+ * be replayed at the same time, need one each.  DASH_ECAPACITY if it is too small: fewer
+ * rows may need more (their rows are cut into more stretches), so ask for each number of rows.
  */
 size_t dash_sample_truncated_workspace_bytes(int32_t n_rows, int32_t vocab, int32_t top_k);
 int dash_sample_truncated(const float* d_logits, int64_t ld, int32_t n_rows, int32_t vocab, const int32_t* d_row_of,

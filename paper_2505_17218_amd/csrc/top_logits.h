@@ -9,7 +9,9 @@
 // cuts below in it, its loop reloaded spilled addresses, and every such reload waits for all loads
 // in flight.
 //
-// The second reads a row's lists into registers, cuts them to the K largest and sorts those in LDS.
+// The second reads a row's lists into registers, cuts them to the K largest and sorts those in LDS:
+// 7.5 us for 8 rows and K = 20, 25 for 2048 and K = 64, 33 for 333 and K = 500, bound by one row's chain of
+// barriers.
 // Lists that do not fit are cut piece by piece, and one that overflowed (a row that holds one value
 // many times, or whose large values the sample misses) sends it over the row itself, a cut whenever
 // the next tile might not fit.  That is slower, never wrong.

@@ -1,5 +1,10 @@
 // The K largest logits of every row, sorted, and the log-sum-exp of the rest: what a teacher's
 // row of 151,936 logits is reduced to for distillation.  Selection: top_logits.h.
+//
+// Bound by reading the row: 2048 rows of 151,936 take 203 us for k = 1 (6.1 TB/s), 236 for k = 64 (210 and 25
+// in the two launches) and 410 for k = 500: what grows with k are the entries above the sampled
+// bound, 9 k of such a row, each put on a list.  With 512 threads and eight tiles in flight k = 64
+// took 300 us, with 512 and four 311.
 #include "kernels.h"
 #include "top_logits.h"
 

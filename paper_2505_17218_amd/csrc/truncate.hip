@@ -25,6 +25,11 @@
 //                left takes another round of both, if there are many rows, and then further passes
 //                of one work-group.
 // Few rows are cut into stretches in the first pass as well, joined by draw_join.
+// Vector instructions bound the first pass, most of them Philox's and the screening's (1024 rows of 151,936
+// without truncation 153 us, the full-vocabulary sampler 130); the later ones are latency.  At top_p = 0.95
+// 64 rows take 25, 12, 10 and 5 us in draw_first, draw_join, draw_second and draw_last; 1024 flat
+// rows 177 us in the first and 8 to 30 in the rest.  With top-k = 64 1024 rows take 110 us in the
+// selection (5.7 TB/s: memory) and 16 in the draw.
 // Masses are float32 exponentials first; only where they are within kMassTol of the border, the sums
 // are repeated in float64, so the decision is that of float64 sums.
 #include <type_traits>
@@ -43,7 +48,10 @@ namespace {
 // <= 28.  Together below 4e-6 for either sum; sums in float64 add nothing.
 constexpr double kMassTol = 1e-5;
 
-constexpr int kDrawTarget = 512;   // work-groups that fill the GPU
+constexpr int kDrawTarget = 512;   // work-groups that fill the GPU: two per CU
+// One per CU where draw_first leaves stretches: in registers for two it spilled a few, and a launch
+// with scratch memory is slow to start (64 rows of 151,936 59 -> 55 us a call, 200 rows 78 -> 70).
+constexpr int kSplitTarget = 256;
 constexpr int kDrawStretch = 4096;  // least entries of a stretch
 
 struct Draw {
@@ -321,7 +329,7 @@ struct Drawing {
 
 // HIST: top_p < 1.  MINP: min_p > 0.  SPLIT: stretches of rows, left for draw_join.
 template <bool UNIT_T, bool HIST, bool MINP, bool SPLIT>
-__global__ void __launch_bounds__(kRowThreads, 8)
+__global__ void __launch_bounds__(kRowThreads, SPLIT ? 4 : 8)
 draw_first(Draw a, RowSplit cut, FirstPart* __restrict__ part, uint32_t* __restrict__ hists, RowState* __restrict__ state,
            int* __restrict__ open) {
     __shared__ uint32_t hist[HIST ? kBins * kCopies : 1];
@@ -647,7 +655,7 @@ struct DrawPlan {
 DrawPlan draw_plan(int rows, int vocab) {
     DrawPlan p;
     const int n = std::max(rows, 1);
-    p.first = split_row(vocab, std::min({kMostParts, kDrawTarget / n, vocab / kDrawStretch}));
+    p.first = split_row(vocab, std::min({kMostParts, kSplitTarget / n, vocab / kDrawStretch}));
     p.most = std::max(1, std::min({kMostCuts, std::max(kDrawTarget / n, 8), vocab / kDrawStretch}));
     const size_t stretches = p.first.n > 1 ? (size_t)n * p.first.n : 0;
     size_t at = 0;

@@ -161,6 +161,12 @@ def test_sample_many_rows(top_k, top_p, min_p):
     _check_sample(l, 0.9, top_k, top_p, min_p, row_of=row_of)
 
 
+@pytest.mark.parametrize("top_k, top_p, min_p", [(0, 0.6, 0.0), (20, 0.9, 0.0), (0, 1.0, 0.2)])
+def test_sample_thousands_of_rows(top_k, top_p, min_p):
+    require_gpu()
+    _check_sample(_rows("normal", 97, 1501, 21), 1.1, top_k, top_p, min_p, row_of=np.arange(3001) % 97)
+
+
 @pytest.mark.parametrize("rows", [3, 260])
 @pytest.mark.parametrize("top_p, min_p", [(0.95, 0.0), (0.4, 0.0), (1.0, 0.1)])
 def test_sample_long_rows(rows, top_p, min_p):
