@@ -220,19 +220,19 @@ struct GradTerms {
 };
 template <int NT>
 DASH_DEV GradTerms grad_terms(const DistillArgs& a, const Teacher<NT>& t, const float (&s)[Teacher<NT>::kOwn],
-                              const Norm& n, float w, int lo, int hi, float (&g)[Teacher<NT>::kOwn]) {
+                              const Norm& n, double w, int lo, int hi, float (&g)[Teacher<NT>::kOwn]) {
     const double T = a.temperature;
     float f = 0.f;
     if (n.z_rest != 0.f) {
         const double q_rest = exp(((double)n.top_rest - (double)n.top) / T) * (double)n.z_rest / (double)n.z;
-        f = (float)((double)w * (q_rest - t.rest_p) / (double)n.z_rest);
+        f = (float)(w * (q_rest - t.rest_p) / (double)n.z_rest);
     }
     if (n.z != n.z) f = n.z;
 #pragma unroll
     for (int e = 0; e < t.kOwn; ++e) {
         g[e] = 0.f;
         if (t.idx[e] >= lo && t.idx[e] < hi)
-            g[e] = (float)((double)w * (exp(((double)s[e] - (double)n.top) / T) / (double)n.z - exp(t.lp(e, T))));
+            g[e] = (float)(w * (exp(((double)s[e] - (double)n.top) / T) / (double)n.z - exp(t.lp(e, T))));
         asm volatile("" : "+v"(g[e]));  // s has arrived before any entry is written
     }
     return {n.top_rest, f};
@@ -253,7 +253,7 @@ DASH_DEV void store_tokens(G* grad, const Teacher<NT>& t, const float (&g)[Teach
 }
 template <int NT, class G>
 DASH_DEV void row_grad(const DistillArgs& a, const float* row, G* grad, int lo, int hi, const Teacher<NT>& t,
-                       const float (&s)[Teacher<NT>::kOwn], const Norm& n, float w) {
+                       const float (&s)[Teacher<NT>::kOwn], const Norm& n, double w) {
     float g[Teacher<NT>::kOwn];
     const GradTerms q = grad_terms(a, t, s, n, w, lo, hi, g);
     __syncthreads();
@@ -367,7 +367,7 @@ distill_grad_k(DistillArgs a, RowSplit cut) {
 #pragma unroll
     for (int e = 0; e < t.kOwn; ++e) s[e] = t.idx[e] >= lo && t.idx[e] < hi ? row[t.idx[e]] : 0.f;
     const Norm n{a.norm[4 * r], a.norm[4 * r + 1], a.norm[4 * r + 2], a.norm[4 * r + 3]};
-    row_grad(a, row, grad, lo, hi, t, s, n, (float)((double)weight / (double)a.temperature));
+    row_grad(a, row, grad, lo, hi, t, s, n, (double)weight / (double)a.temperature);
 }
 
 // Loss and gradient of a row by one work-group, a CU to itself.  Both passes need the row, 608 KB of
@@ -435,7 +435,7 @@ distill_loss_grad_k(DistillArgs a) {
     const float loss = row_loss(a, t, s, sum, sh.twice, sh, n);
     if (threadIdx.x == 0) a.loss[r] = loss;
     float g[t.kOwn];
-    const GradTerms q = grad_terms(a, t, s, n, (float)((double)weight / (double)a.temperature), 0, a.vocab, g);
+    const GradTerms q = grad_terms(a, t, s, n, (double)weight / (double)a.temperature, 0, a.vocab, g);
     __syncthreads();  // every thread has its tokens' logits: entries may be written
     auto write = [&](const f32x4_t& l, int i) {
         float v[4];

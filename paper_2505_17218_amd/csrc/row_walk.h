@@ -101,9 +101,11 @@ __host__ __device__ inline float exp2_scale(double temperature) {
     return (float)fmin(1.4426950408889634 / temperature, (double)FLT_MAX);
 }
 // What rounding that factor to float32 left out: with it exponents are right to their own rounding.
+// Nothing above 2^24 (T < 8.6e-8), where the largest float times it could overflow against the product
+// with the factor itself; it is worth 2^-25 of an exponent.
 __host__ __device__ inline float exp2_scale_low(double temperature) {
     const double s = 1.4426950408889634 / temperature;
-    return s < (double)FLT_MAX ? (float)(s - (double)(float)s) : 0.f;
+    return s <= 16777216.0 ? (float)(s - (double)(float)s) : 0.f;
 }
 
 // A thread's sum of e^((x - ref) / T).  ref follows the entries lazily: it is raised to a group's

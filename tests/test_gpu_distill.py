@@ -152,6 +152,29 @@ def test_large(rows, V, k):
     _check(s, v, i, None, 1.0, None, torch.bfloat16)
 
 
+@pytest.mark.parametrize("T", [1e-30, 1e-3, 1e3, 1e30])
+def test_small_and_large_temperatures(T):
+    require_gpu()
+    t, s, rng = _pair(3, 3001, 14)
+    v, i, rest = _teacher(t, 20, T)
+    w = rng.random(3).astype(np.float32)
+    _check(s, v, i, rest, T, w)
+    _check(s, v, i, None, T, w)
+
+
+def test_a_gradient_of_zero_at_a_denormal_temperature():
+    """1 / T is above the float32 range, the gradient of an equal student still 0."""
+    require_gpu()
+    t, _, _ = _pair(3, 3001, 15)
+    v, i, _ = _teacher(t, 20, 1.0)
+    vd, id_ = _f32(v), dev_i32(i)
+    loss, norm = engine.distill_loss(_f32(t), vd, id_, None, 1e-39)
+    grad = engine.distill_grad(_f32(t), vd, id_, norm, None, 1e-39)
+    both_loss, both = engine.distill_loss_grad(_f32(t), vd, id_, None, 1e-39)
+    for x in (loss, grad, both_loss, both):
+        assert not x.any()
+
+
 def test_sure_students():
     """The teacher's tokens hold all but 1e-30 of the student's mass, or the other tokens do: nothing cancels, and what is
     left of p_rest is spread over the others."""
