@@ -635,6 +635,7 @@ draw_last(Draw a, int rows, RowState* __restrict__ state, int* __restrict__ open
                 }
                 before = draw_before<kLater, UNIT_T>(a, b, row, 0, a.vocab, w, &floor_s, best, red_d, s, next);
             }
+            if constexpr (!LAST) __syncthreads();  // every wave has read the row's state
             if (threadIdx.x != 0) continue;
             if (!ended) {
                 state[b] = w;
