@@ -179,6 +179,8 @@ def test_small_and_large_temperatures():
     require_gpu()
     l = _rows("normal", 4, 3001, 8)
     for T in (1e-3, 1e-30, 1e-38, 1e3, 1e30):
+        if T > 1e-38:  # (a rest of that temperature is above the float32 range)
+            _check_top(l, 25, T)
         for top_k, top_p, min_p in ((0, 0.9, 0.0), (30, 0.9, 0.0), (0, 1.0, 0.5)):
             _check_sample(l, T, top_k, top_p, min_p)
 
@@ -303,3 +305,50 @@ def test_other_stream_and_graph():
         torch.cuda.synchronize()
         for a, b in zip(calls(), held):
             assert torch.equal(a, b)
+
+
+def test_calls_at_once_on_two_streams():
+    """Calls that overlap in time have workspaces of their own: 20 of each kind on two streams, other rows on either."""
+    require_gpu()
+    sides = []
+    for s in range(2):
+        l = torch.from_numpy(_rows("normal", 300, 20011, 22 + s)).cuda()
+        teacher = torch.from_numpy(_rows("peak", 300, 20011, 24 + s)).cuda()
+        sides.append((l, teacher, dev_i32(np.arange(300) + s), torch.cuda.Stream()))
+
+    def calls(l, teacher, uid):
+        v, i, rest = engine.top_logits(teacher, 64, 1.0)
+        return (v, i, rest, *engine.distill_loss_grad(l, v, i, rest), *engine.sample_truncated(l, uid, uid, 0.9, 3, 0, 0.6),
+                *engine.sample_truncated(l, uid, uid, 0.9, 3, 600, 0.9))
+
+    want = [calls(*s[:3]) for s in sides]
+    torch.cuda.synchronize()
+    got = [[], []]
+    for _ in range(20):
+        for k, s in enumerate(sides):
+            with torch.cuda.stream(s[3]):
+                got[k].append(calls(*s[:3]))
+    torch.cuda.synchronize()
+    for k in range(2):
+        for g in got[k]:
+            assert all(torch.equal(a, b) for a, b in zip(g, want[k]))
+
+
+def test_two_graphs_replayed_in_turn():
+    require_gpu()
+    graphs = []
+    for s in range(2):
+        l = torch.from_numpy(_rows("normal", 40, 30011, 26 + s)).cuda()
+        uid = dev_i32(np.arange(40) + s)
+        run = lambda l=l, uid=uid: (*engine.top_logits(l, 700, 1.0), *engine.sample_truncated(l, uid, uid, 1.0, 5, 0, 0.5))
+        run()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            held = run()
+        graphs.append((graph, held, run))
+    for _ in range(4):
+        for graph, held, run in graphs:
+            graph.replay()
+            want = run()
+            torch.cuda.synchronize()
+            assert all(torch.equal(a, b) for a, b in zip(held, want))
