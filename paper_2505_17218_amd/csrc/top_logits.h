@@ -370,7 +370,8 @@ DASH_DEV int top_finish(TopShared<NT, PER>& sh, TopState& st, int k, int p, floa
     __syncthreads();
     if constexpr (NT <= kTopSmall) {
         // A word's place is the number of larger ones (words differ; zeros fill what is left):
-        // NT / p threads per word count over a share of the words each.
+        // NT / p threads per word count over a share of the words each.  (Quadratic: 333 rows and K = 500 take 103 us
+        // by counting, 96 by the exchanges below.)
         const int i = (int)threadIdx.x & (p - 1), share = (int)threadIdx.x / p, len = p * p / NT;
         const uint64_t mine = sh.c[i];
         int place = 0;
