@@ -27,7 +27,7 @@
 // Few rows are cut into stretches in the first pass as well, joined by draw_join.
 // Vector instructions bound the first pass, most of them Philox's and the screening's (1024 rows of 151,936
 // without truncation 153 us, the full-vocabulary sampler 130); the later ones are latency.  At top_p = 0.95
-// 64 rows take 25, 12, 10 and 5 us in draw_first, draw_join, draw_second and draw_last; 1024 flat
+// 64 rows take 23, 11, 13 and 5 us in draw_first, draw_join, draw_second and draw_last; 1024 flat
 // rows 177 us in the first and 8 to 30 in the rest.  With top-k = 64 1024 rows take 110 us in the
 // selection (5.7 TB/s: memory) and 16 in the draw.
 // Masses are float32 exponentials first; only where they are within kMassTol of the border, the sums
