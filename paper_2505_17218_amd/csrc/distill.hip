@@ -455,16 +455,20 @@ RowSplit loss_split(int rows, int vocab) {
     return split_row(vocab, std::min({64, kDistillTarget / std::max(rows, 1), vocab / kDistillStretch}));
 }
 
-// One work-group for loss and gradient of a row: where there are rows for every CU, and the row's
-// marks are in LDS at once.
-bool fused(int rows, int vocab) { return loss_split(rows, vocab).n == 1 && vocab <= kStretch; }
+// One work-group for loss and gradient of a row: where there are rows for every CU, the row's marks are in
+// LDS at once, and what is not read again outweighs that a CU has one work-group instead of
+// four.  2048 rows, pair of launches / one: 32,768 entries 159 / 164 us in float32 and 133 / 159 in bf16,
+// 50,257 263 / 237 and 216 / 216, 80,000 360 / 311 and 293 / 282, 151,936 721 / 545 and 556 / 438; 706 47 / 87.
+bool fused(int rows, int vocab, bool bf16) {
+    return loss_split(rows, vocab).n == 1 && vocab >= (bf16 ? 1 << 16 : 40960) && vocab <= kStretch;
+}
 
 }  // namespace
 
 size_t distill_workspace_bytes(int rows, int vocab) {
     const RowSplit cut = loss_split(rows, vocab);
     const size_t parts = cut.n == 1 ? 0 : (size_t)rows * cut.n * sizeof(DistillPart);
-    return parts + (fused(rows, vocab) ? 0 : (size_t)rows * 4 * sizeof(float));
+    return parts + (fused(rows, vocab, true) ? 0 : (size_t)rows * 4 * sizeof(float));  // (float32 needs none where bf16 does not)
 }
 
 hipError_t launch_distill_loss(DistillArgs a, void* ws, hipStream_t st) {
@@ -495,7 +499,7 @@ hipError_t launch_distill_grad(DistillArgs a, hipStream_t st) {
 hipError_t launch_distill_loss_grad(DistillArgs a, void* ws, hipStream_t st) {
     if (a.rows <= 0) return hipSuccess;
     const RowSplit cut = loss_split(a.rows, a.vocab);
-    if (!fused(a.rows, a.vocab)) {
+    if (!fused(a.rows, a.vocab, a.grad_bf16)) {
         a.norm = (float*)((DistillPart*)ws + (cut.n == 1 ? 0 : (size_t)a.rows * cut.n));
         if (hipError_t e = launch_distill_loss(a, ws, st)) return e;
         return launch_distill_grad(a, st);

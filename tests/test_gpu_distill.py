@@ -114,6 +114,8 @@ def test_sizes(V):
 
 
 @pytest.mark.parametrize("rows, V, k, dtype", [
+    (513, 40960, 20, torch.float32), (520, 50257, 30, torch.float32), (513, 40959, 30, torch.float32),
+    (513, 65536, 30, torch.bfloat16), (520, 65535, 30, torch.bfloat16),
     (513, 90112, 40, torch.float32), (513, 90115, 40, torch.bfloat16), (513, 118784, 1024, torch.bfloat16),
     (514, 118785, 300, torch.float32), (520, 151936, 64, torch.bfloat16), (520, 151933, 64, torch.float32),
     (513, (1 << 18) + 6, 64, torch.bfloat16), (1100, 8200, 64, torch.float32), (3000, 300, 20, torch.bfloat16)])
