@@ -365,8 +365,11 @@ draw_first(Draw a, RowSplit cut, FirstPart* __restrict__ part, uint32_t* __restr
             if (m == -INFINITY) return;
             ref = m;
             if (HIST && fabsf(m * a.scale) < 16384.f) {  // (whole octaves: stretches share a grid of bins)
-                bins_at = rintf(m * a.scale);
-                ref = octaves(bins_at, a.temperature);
+                const float at = rintf(m * a.scale), whole = octaves(at, a.temperature);
+                if (fabsf(whole) < INFINITY) {  // (rounded up, it may lie past the largest float)
+                    bins_at = at;
+                    ref = whole;
+                }
             }
         },
         [&](f32x4_t l, int i) {
