@@ -216,7 +216,7 @@ DASH_DEV void store1(bf16_t* p, float v) { *p = f2bf(v); }
 // Gradient of a row's entries [lo, hi), w = its weight / T.  grad may be the row itself: a thread reads
 // its entries before it writes them, and the teacher's tokens (s, read before) are written last.
 struct GradTerms {
-    float top_rest, f;  // an other token's gradient: e^((s - top_rest) / T) f
+    float half, f;  // half: top_rest / 2; an other token's gradient: e^((s - top_rest) / T) f
 };
 template <int NT>
 DASH_DEV GradTerms grad_terms(const DistillArgs& a, const Teacher<NT>& t, const float (&s)[Teacher<NT>::kOwn],
@@ -235,12 +235,12 @@ DASH_DEV GradTerms grad_terms(const DistillArgs& a, const Teacher<NT>& t, const 
             g[e] = (float)(w * (exp(((double)s[e] - (double)n.top) / T) / (double)n.z - exp(t.lp(e, T))));
         asm volatile("" : "+v"(g[e]));  // s has arrived before any entry is written
     }
-    return {n.top_rest, f};
+    return {0.5f * n.top_rest, f};
 }
 DASH_DEV void grad4(const DistillArgs& a, const GradTerms& q, const f32x4_t& l, float (&v)[4]) {
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-        const float d = l[j] - q.top_rest;
+        const float d = half_gap(l[j], q.half);
         v[j] = __builtin_amdgcn_exp2f(__builtin_fmaf(d, a.scale, fmaxf(d, -FLT_MAX) * a.scale_low)) * q.f;
     }
 }
@@ -339,7 +339,7 @@ distill_join_k(DistillArgs a, const DistillPart* __restrict__ part, int parts) {
     ExpSum sum;
     if (p.z != 0.0) {
         sum.z = p.z;
-        sum.ref = p.ref;
+        sum.half = 0.5f * p.ref;
     }
     Norm n;
     const float loss = row_loss(a, t, s, sum, __syncthreads_or(p.twice), sh, n);

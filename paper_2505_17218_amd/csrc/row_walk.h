@@ -96,40 +96,48 @@ inline RowSplit split_row(int vocab, int n) {
     return {(vocab + len - 1) / len, len};
 }
 
-// log2(e) / T, so that e^((x - m) / T) = 2^((x - m) scale); finite for every T > 0 (0 times it stays 0).
+// Exponents are taken of half the difference of two logits: the whole one may lie past the largest
+// float, and at T = 10^38 be worth a few octaves all the same.  Halving is exact (but for
+// denormals) and one instruction with the difference, so the product below is that of the whole
+// difference and log2(e) / T, bit for bit.
+DASH_DEV float half_gap(float x, float half) { return __builtin_fmaf(x, 0.5f, -half); }
+// 2 log2(e) / T, so that e^((x - m) / T) = 2^(half_gap(x, m / 2) scale); finite for every T > 0 (0 times it
+// stays 0).
 __host__ __device__ inline float exp2_scale(double temperature) {
-    return (float)fmin(1.4426950408889634 / temperature, (double)FLT_MAX);
+    return (float)fmin(2.0 * 1.4426950408889634 / temperature, (double)FLT_MAX);
 }
 // What rounding that factor to float32 left out: with it exponents are right to their own rounding.
-// Nothing above 2^24 (T < 8.6e-8), where the largest float times it could overflow against the product
+// Nothing above 2^25 (T < 8.6e-8), where the largest float times it could overflow against the product
 // with the factor itself; it is worth 2^-25 of an exponent.
 __host__ __device__ inline float exp2_scale_low(double temperature) {
-    const double s = 1.4426950408889634 / temperature;
-    return s <= 16777216.0 ? (float)(s - (double)(float)s) : 0.f;
+    const double s = 2.0 * 1.4426950408889634 / temperature;
+    return s <= 33554432.0 ? (float)(s - (double)(float)s) : 0.f;
 }
 
 // A thread's sum of e^((x - ref) / T).  ref follows the entries lazily: it is raised to a group's
 // maximum only where that is 2^40 above it, so that most groups need no rescale and float32 terms
 // neither overflow nor lose what matters; the sum itself is float64 (a thread may add 2^18 terms).
 struct ExpSum {
-    float ref = -FLT_MAX;
+    float half = -0.5f * FLT_MAX;  // ref / 2
     double z = 0.0;
+    DASH_DEV float ref() const { return 2.f * half; }
 };
 
 // Four terms; -inf adds nothing, NaN and +inf make the sum NaN.  LOW: with the scale's low part.
 template <bool LOW>
 DASH_DEV void exp_push4(ExpSum& s, const f32x4_t& x, float m4, float scale, float low = 0.f) {
-    const bool far = (m4 - s.ref) * scale > 40.f;
+    const float above = half_gap(m4, s.half) * scale;
+    const bool far = above > 40.f;
     if (__any(far)) {
         if (far) {
-            s.z *= (double)__builtin_amdgcn_exp2f((s.ref - m4) * scale);
-            s.ref = m4;
+            s.z *= (double)__builtin_amdgcn_exp2f(-above);
+            s.half = 0.5f * m4;
         }
     }
     float e[4];
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-        const float d = x[j] - s.ref;
+        const float d = half_gap(x[j], s.half);
         // (the low product is kept finite: -inf times a low part of either sign or zero)
         const float y = LOW ? __builtin_fmaf(d, scale, fmaxf(d, -FLT_MAX) * low) : d * scale;
         e[j] = __builtin_amdgcn_exp2f(y);
@@ -139,11 +147,11 @@ DASH_DEV void exp_push4(ExpSum& s, const f32x4_t& x, float m4, float scale, floa
 
 // One finite term.
 DASH_DEV void exp_push1(ExpSum& s, float x, float scale) {
-    if (x > s.ref) {
-        s.z *= (double)__builtin_amdgcn_exp2f((s.ref - x) * scale);
-        s.ref = x;
+    if (x > s.ref()) {
+        s.z *= (double)__builtin_amdgcn_exp2f(-half_gap(x, s.half) * scale);
+        s.half = 0.5f * x;
     }
-    s.z += (double)__builtin_amdgcn_exp2f((x - s.ref) * scale);
+    s.z += (double)__builtin_amdgcn_exp2f(half_gap(x, s.half) * scale);
 }
 
 // Inclusive sum over the threads up to this one (of NT), and the total.
@@ -199,9 +207,9 @@ DASH_DEV float block_max_f(float v, float* red) {
 // Sum over the work-group's threads of e^((l - ref) / T) (0: nothing), and ref.
 template <int NT = kRowThreads>
 DASH_DEV double block_exp_sum(const ExpSum& s, double temperature, float* red_f, double* red_d, float& ref) {
-    ref = block_max_f<NT>(s.z > 0.0 ? s.ref : -FLT_MAX, red_f);
+    ref = block_max_f<NT>(s.z > 0.0 ? s.ref() : -FLT_MAX, red_f);
     // (a NaN sum stays one)
-    return block_sum_d<NT>(s.z == 0.0 ? 0.0 : s.z * exp(((double)s.ref - (double)ref) / temperature), red_d);
+    return block_sum_d<NT>(s.z == 0.0 ? 0.0 : s.z * exp(((double)s.ref() - (double)ref) / temperature), red_d);
 }
 
 }  // namespace dash

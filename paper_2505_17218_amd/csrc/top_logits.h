@@ -169,9 +169,9 @@ DASH_DEV void top_turn_away(TopShared<NT, PER>& sh, TopState& st, unsigned out, 
     __syncthreads();
     const unsigned top = sh.evict_ref;
     if (!top) return;
-    const float ref = top_value(top);
+    const float ref = top_value(top), half = 0.5f * ref;
     uint64_t z = 0;
-    each([&](uint64_t w) { z += (uint64_t)(__builtin_amdgcn_exp2f((word_value(w) - ref) * scale) * kEvictOne); });
+    each([&](uint64_t w) { z += (uint64_t)(__builtin_amdgcn_exp2f(half_gap(word_value(w), half) * scale) * kEvictOne); });
     if (__any(z != 0)) {
 #pragma unroll
         for (int o = 32; o >= 1; o >>= 1) z += (uint64_t)__shfl_xor((long long)z, o, 64);
@@ -180,11 +180,12 @@ DASH_DEV void top_turn_away(TopShared<NT, PER>& sh, TopState& st, unsigned out, 
     __syncthreads();
     if (threadIdx.x == 0) {
         const double zd = (double)sh.evict_z / (double)kEvictOne;
-        if (ref > st.rest.ref) {
-            st.rest.z = st.rest.z * exp2((double)(st.rest.ref - ref) * (double)scale) + zd;
-            st.rest.ref = ref;
+        const double above = (double)half_gap(ref, st.rest.half) * (double)scale;
+        if (above > 0.0) {
+            st.rest.z = st.rest.z * exp2(-above) + zd;
+            st.rest.half = half;
         } else {
-            st.rest.z += zd * exp2((double)(ref - st.rest.ref) * (double)scale);
+            st.rest.z += zd * exp2(above);
         }
     }
 }
@@ -267,7 +268,7 @@ DASH_DEV void top_gather(TopShared<NT, PER>& sh, TopState& st, const TopParts& p
         const TopPart mine = part[lane];
         n = mine.n;
         if (threadIdx.x < 64 && mine.z > 0.0) {
-            st.rest.ref = mine.ref;
+            st.rest.half = 0.5f * mine.ref;
             st.rest.z = mine.z;
         }
     }

@@ -237,7 +237,7 @@ DASH_DEV void settle(const Draw& a, int b, const float* row, int tok, float top,
                 const int whole = block_reduce(from >= a.top_p * z + tol ? (int)threadIdx.x : 0, sh.red_i, most);
                 r.sure = last + 2;
                 r.border = whole - 1;
-                const int at = bin_of(__builtin_amdgcn_exp2f((r.l - bin_ref) * a.scale));
+                const int at = bin_of(__builtin_amdgcn_exp2f(half_gap(r.l, 0.5f * bin_ref) * a.scale));
                 done = reaches && at >= r.sure;
                 r.unsure = reaches && at >= r.border;
             }
@@ -350,7 +350,7 @@ draw_first(Draw a, RowSplit cut, FirstPart* __restrict__ part, uint32_t* __restr
     __syncthreads();
     const float min_gap = MINP ? (float)((double)a.temperature * a.log_min_p) : 0.f;
     const int copy = threadIdx.x & (kCopies - 1);
-    float ref = -FLT_MAX, bins_at = NAN, top = -INFINITY;
+    float half = -0.5f * FLT_MAX, bins_at = NAN, top = -INFINITY;  // half: of the reference
     double z = 0.0;
     walk_row<2, true, false>(
         row, SPLIT ? n * cut.len : 0, SPLIT ? min(a.vocab, (n + 1) * cut.len) : a.vocab,
@@ -363,12 +363,12 @@ draw_first(Draw a, RowSplit cut, FirstPart* __restrict__ part, uint32_t* __restr
                 for (int j = 0; j < 4; ++j) m = fmaxf(m, buf[d][j] < INFINITY ? buf[d][j] : -INFINITY);
             m = block_max_f(m, red_f);
             if (m == -INFINITY) return;
-            ref = m;
-            if (HIST && fabsf(m * a.scale) < 16384.f) {  // (whole octaves: stretches share a grid of bins)
-                const float at = rintf(m * a.scale), whole = octaves(at, a.temperature);
+            half = 0.5f * m;
+            if (HIST && fabsf(half * a.scale) < 16384.f) {  // (whole octaves: stretches share a grid of bins)
+                const float at = rintf(half * a.scale), whole = octaves(at, a.temperature);
                 if (fabsf(whole) < INFINITY) {  // (rounded up, it may lie past the largest float)
                     bins_at = at;
-                    ref = whole;
+                    half = 0.5f * whole;
                 }
             }
         },
@@ -377,17 +377,18 @@ draw_first(Draw a, RowSplit cut, FirstPart* __restrict__ part, uint32_t* __restr
             const float m4 = max4(l);
             if (!__any(m4 > -INFINITY)) return;
             top = fmaxf(top, m4);
-            const bool far = (m4 - ref) * a.scale >= (HIST ? (float)kBinsAbove : 40.f);
+            const float above = half_gap(m4, half) * a.scale;
+            const bool far = above >= (HIST ? (float)kBinsAbove : 40.f);
             if (__any(far)) {  // as in exp_push4; the histogram is void then
                 if (far) {
-                    z *= (double)__builtin_amdgcn_exp2f((ref - m4) * a.scale);
-                    ref = m4;
+                    z *= (double)__builtin_amdgcn_exp2f(-above);
+                    half = 0.5f * m4;
                     far_s = 1;
                 }
             }
             float e[4];
 #pragma unroll
-            for (int j = 0; j < 4; ++j) e[j] = __builtin_amdgcn_exp2f((l[j] - ref) * a.scale);
+            for (int j = 0; j < 4; ++j) e[j] = __builtin_amdgcn_exp2f(half_gap(l[j], half) * a.scale);
             z += (double)((e[0] + e[1]) + (e[2] + e[3]));
             if constexpr (HIST) {
 #pragma unroll
@@ -413,7 +414,7 @@ draw_first(Draw a, RowSplit cut, FirstPart* __restrict__ part, uint32_t* __restr
         [](int) { return false; });
     block_best(draw.s, draw.i, best);
     top = block_max_f(top, red_f);
-    const float at = block_max_f(z > 0.0 ? ref : -FLT_MAX, red_f);
+    const float ref = 2.f * half, at = block_max_f(z > 0.0 ? ref : -FLT_MAX, red_f);
     const double T = a.temperature;
     z = block_sum_d(z > 0.0 ? z * exp(((double)ref - (double)at) / T) : 0.0, settled.red);
     if (far_s) bins_at = NAN;
@@ -497,6 +498,7 @@ DASH_DEV double draw_before(const Draw& a, int b, const float* row, int lo, int 
     Drawing<UNIT_T> draw(a, b, floor_s);
     __syncthreads();
     double mass = 0.0;
+    const float half_top = 0.5f * w.top, half_bins = 0.5f * w.bin_ref;
     // the least exponential of the border's bin (bin 0 holds all below it, too)
     const float border = w.bin_ref == w.bin_ref && w.border > 0 ? __uint_as_float((kBinBase + w.border) << 18) : 0.f;
     walk_row<2, false, NT>(row, lo, hi, [&](f32x4_t l, int i) {
@@ -506,12 +508,12 @@ DASH_DEV double draw_before(const Draw& a, int b, const float* row, int lo, int 
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
             l[j] = l[j] > w.l || (l[j] == w.l && i + j < w.tok) ? l[j] : -INFINITY;
-            e[j] = __builtin_amdgcn_exp2f((l[j] - w.top) * a.scale);
+            e[j] = __builtin_amdgcn_exp2f(half_gap(l[j], half_top) * a.scale);
         }
         mass += (double)((e[0] + e[1]) + (e[2] + e[3]));
 #pragma unroll
         for (int j = 0; j < 4; ++j)
-            l[j] = l[j] < w.low || __builtin_amdgcn_exp2f((l[j] - w.bin_ref) * a.scale) < border ? -INFINITY : l[j];
+            l[j] = l[j] < w.low || __builtin_amdgcn_exp2f(half_gap(l[j], half_bins) * a.scale) < border ? -INFINITY : l[j];
         if (__any(max4(l) > -INFINITY)) draw.score4(a, l, i, true);
     });
     s = draw.s;
@@ -630,7 +632,7 @@ draw_last(Draw a, int rows, RowState* __restrict__ state, int* __restrict__ open
                 w.tok = next;
                 w.l = row[next];
                 if (a.top_p >= 1.0 || kept_by_own_mass(a, w.l, w.top, w.z)) break;
-                if (w.bin_ref == w.bin_ref && bin_of(__builtin_amdgcn_exp2f((w.l - w.bin_ref) * a.scale)) >= w.sure) break;
+                if (w.bin_ref == w.bin_ref && bin_of(__builtin_amdgcn_exp2f(half_gap(w.l, 0.5f * w.bin_ref) * a.scale)) >= w.sure) break;
                 w.unsure = 1;
                 if constexpr (!LAST) {
                     ended = false;

@@ -6,8 +6,12 @@ import numpy as np
 import pytest
 import torch
 
-from gpu_util import require_gpu
-from test_gpu_truncated import _check_sample
+from oracle import distill
+from paper_2505_17218_amd import engine
+
+from gpu_util import dev_i32, require_gpu
+from test_gpu_distill import _check_grad, _check_loss, _f32, _teacher
+from test_gpu_truncated import _check_sample, _check_top
 
 pytestmark = pytest.mark.gpu
 
@@ -26,3 +30,51 @@ def test_top_p_next_to_the_largest_float(T, rows, V):
     l[:, V // 3] = HIGH
     for top_p, min_p in ((0.9, 0.0), (0.3, 0.0), (0.95, 0.05), (1.0, 0.1)):
         _check_sample(l, T, 0, top_p, min_p, row_of=np.arange(rows) % l.shape[0])
+
+
+def _wide(rows, V, seed):
+    l = np.random.default_rng([seed, V]).uniform(-1, 1, (rows, V)).astype(np.float32) * np.float32(3.3e38)
+    l[:, V // 2] = HIGH
+    l[0, V // 5] = -HIGH
+    l[-1, 1:] = -HIGH  # one token far above all others
+    return l
+
+
+@pytest.mark.parametrize("rows, V", [(5, 3001), (4, 20001), (600, 9001)])
+@pytest.mark.parametrize("T", [1e37, 4e37, 1e38, 3.4e38])
+def test_draws_over_the_whole_range(T, rows, V):
+    """Differences of two logits are up to twice the largest float32, and still only a few T."""
+    require_gpu()
+    l = _wide(min(rows, 7), V, 32)
+    for top_k, top_p, min_p in ((0, 0.9, 0.0), (0, 1.0, 0.0), (0, 0.95, 0.3), (0, 1.0, 0.2), (30, 0.9, 0.0), (700, 0.6, 0.0)):
+        _check_sample(l, T, top_k, top_p, min_p, row_of=np.arange(rows) % l.shape[0])
+
+
+@pytest.mark.parametrize("V", [3001, 20001])
+@pytest.mark.parametrize("T", [1e37, 4e37, 1e38, 3.4e38])
+def test_largest_logits_over_the_whole_range(T, V):
+    require_gpu()
+    l = _wide(5, V, 33)
+    l[2, :V // 2] = -HIGH
+    for k in (1, 50, 1000):
+        _check_top(l, k, T)
+
+
+@pytest.mark.parametrize("rows, V, k", [(5, 3001, 20), (4, 20001, 30), (520, 40961, 30)])
+@pytest.mark.parametrize("T", [1e37, 4e37, 1e38, 3.4e38])
+def test_distillation_over_the_whole_range(T, rows, V, k):
+    require_gpu()
+    few = min(rows, 5)
+    t, s = _wide(few, V, 34), _wide(few, V, 35)
+    v, i, rest = _teacher(t, k, T)
+    w = np.full(few, T / 8, np.float32)
+    at = np.arange(rows) % few
+    dev, vd, id_, rd, wd = _f32(s[at]), _f32(v[at]), dev_i32(i[at]), _f32(rest[at]), _f32(w[at])
+    loss, norm = engine.distill_loss(dev, vd, id_, rd, T)
+    grad = engine.distill_grad(dev, vd, id_, norm, rd, T, wd)
+    both_loss, both = engine.distill_loss_grad(dev, vd, id_, rd, T, wd)
+    assert torch.equal(loss, both_loss) and torch.equal(grad, both)
+    for r in [*range(few), rows - 1]:
+        want = distill.row(s[at[r]], v[at[r]], i[at[r]], rest[at[r]], T)
+        _check_loss(loss[r].item(), want, (r, V, T))
+        _check_grad(grad[r].double().cpu().numpy(), want, T, float(w[at[r]]), torch.float32, (r, V, T))
