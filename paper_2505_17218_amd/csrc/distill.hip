@@ -216,16 +216,22 @@ DASH_DEV void store1(bf16_t* p, float v) { *p = f2bf(v); }
 // Gradient of a row's entries [lo, hi), w = its weight / T.  grad may be the row itself: a thread reads
 // its entries before it writes them, and the teacher's tokens (s, read before) are written last.
 struct GradTerms {
-    float half, f;  // half: top_rest / 2; an other token's gradient: e^((s - top_rest) / T) f
+    float half, f, up;  // half: top_rest / 2; an other token's gradient: e^((s - top_rest) / T) 2^up f
 };
 template <int NT>
 DASH_DEV GradTerms grad_terms(const DistillArgs& a, const Teacher<NT>& t, const float (&s)[Teacher<NT>::kOwn],
                               const Norm& n, double w, int lo, int hi, float (&g)[Teacher<NT>::kOwn]) {
     const double T = a.temperature;
-    float f = 0.f;
+    double f = 0.0;
+    int up = 0;
     if (n.z_rest != 0.f) {
         const double q_rest = exp(((double)n.top_rest - (double)n.top) / T) * (double)n.z_rest / (double)n.z;
-        f = (float)(w * (q_rest - t.rest_p) / (double)n.z_rest);
+        f = w * (q_rest - t.rest_p) / (double)n.z_rest;
+        // A factor past the largest float (w is, at T < 3e-39) would make 0 times it NaN: its powers of two join the exponent.
+        if (fabs(f) > (double)FLT_MAX && fabs(f) < (double)INFINITY) {
+            up = ilogb(f) - 126;
+            f = ldexp(f, -up);
+        }
     }
     if (n.z != n.z) f = n.z;
 #pragma unroll
@@ -235,13 +241,13 @@ DASH_DEV GradTerms grad_terms(const DistillArgs& a, const Teacher<NT>& t, const 
             g[e] = (float)(w * (exp(((double)s[e] - (double)n.top) / T) / (double)n.z - exp(t.lp(e, T))));
         asm volatile("" : "+v"(g[e]));  // s has arrived before any entry is written
     }
-    return {0.5f * n.top_rest, f};
+    return {0.5f * n.top_rest, (float)f, (float)up};
 }
 DASH_DEV void grad4(const DistillArgs& a, const GradTerms& q, const f32x4_t& l, float (&v)[4]) {
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
         const float d = half_gap(l[j], q.half);
-        v[j] = __builtin_amdgcn_exp2f(__builtin_fmaf(d, a.scale, fmaxf(d, -FLT_MAX) * a.scale_low)) * q.f;
+        v[j] = __builtin_amdgcn_exp2f(__builtin_fmaf(d, a.scale, __builtin_fmaf(fmaxf(d, -FLT_MAX), a.scale_low, q.up))) * q.f;
     }
 }
 template <int NT, class G>

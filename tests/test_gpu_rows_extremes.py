@@ -1,4 +1,5 @@
-"""The operators on rows of logits at temperatures near the largest float32, over logits that use the type's whole range.
+"""The operators on rows of logits at the ends of the float32 range: temperatures near the largest float32 over logits that
+use the whole range, and weights that the temperature carries past it.
 
 Bounds as in test_gpu_truncated.py and test_gpu_distill.py: they count roundings relative to an exponent's size, so they do
 not depend on the scale of logits and temperature."""
@@ -10,7 +11,7 @@ from oracle import distill
 from paper_2505_17218_amd import engine
 
 from gpu_util import dev_i32, require_gpu
-from test_gpu_distill import _check_grad, _check_loss, _f32, _teacher
+from test_gpu_distill import _check_grad, _check_loss, _f32, _pair, _teacher
 from test_gpu_truncated import _check_sample, _check_top
 
 pytestmark = pytest.mark.gpu
@@ -78,3 +79,32 @@ def test_distillation_over_the_whole_range(T, rows, V, k):
         want = distill.row(s[at[r]], v[at[r]], i[at[r]], rest[at[r]], T)
         _check_loss(loss[r].item(), want, (r, V, T))
         _check_grad(grad[r].double().cpu().numpy(), want, T, float(w[at[r]]), torch.float32, (r, V, T))
+
+
+@pytest.mark.parametrize("rows, V", [(4, 3001), (4, 20001), (520, 40961)])
+@pytest.mark.parametrize("T, weight", [(1e-39, 6.0), (1e-38, 6000.0), (0.1, 3e38)])
+def test_weights_over_the_temperature_past_the_float_range(T, weight, rows, V):
+    """weight / T times a row's mass difference is above the largest float32: entries whose share is 0 (masked ones among
+    them) have gradient 0, those in between what the product gives."""
+    require_gpu()
+    few = min(rows, 4)
+    t, s, rng = _pair(few, V, 36)
+    s[:, rng.random(V) < 0.3] = -np.inf
+    v, i, _ = _teacher(t, 20, 1.0)
+    s[1, np.flatnonzero(~np.isin(np.arange(V), i[1]))[V // 2]] = 30.0  # (not the teacher's)
+    w = np.full(few, weight, np.float32)
+    at = np.arange(rows) % few
+    dev, vd, id_, wd = _f32(s[at]), _f32(v[at]), dev_i32(i[at]), _f32(w[at])
+    _, norm = engine.distill_loss(dev, vd, id_, None, T)
+    grad = engine.distill_grad(dev, vd, id_, norm, None, T, wd)
+    _, both = engine.distill_loss_grad(dev, vd, id_, None, T, wd)
+    assert torch.equal(grad, both)
+    for r in [*range(few), rows - 1]:
+        want = distill.row(s[at[r]], v[at[r]], i[at[r]], None, T)
+        got = grad[r].double().cpu().numpy()
+        with np.errstate(over="ignore"):
+            past = np.isinf((want.grad * float(w[at[r]])).astype(np.float32))  # past the float32 range themselves
+        assert past.any() or at[r] != 1
+        np.testing.assert_array_equal(got[past], np.sign(want.grad[past]) * np.inf)
+        want.grad[past] = got[past] = 0.0
+        _check_grad(got, want, T, float(w[at[r]]), torch.float32, (r, V, T))
