@@ -36,8 +36,9 @@ DASH_DEV f32x4_t load_row4(const float* row, int i) {
 // these before f does; where there are fewer whole tiles than DEPTH, the last one (the partial one,
 // if there is none) fills the places of the missing.  round(t) is called after the t-th DEPTH tiles
 // (1, 2, ...) and ends the walk by returning true.  STREAM: rows that nothing reads again.
+// f may write the entries that it was called with in their place, so row is not __restrict__.
 template <int DEPTH, bool STRIPES, bool STREAM, int NT = kRowThreads, class START, class F, class ROUND>
-DASH_DEV void walk_row(const float* __restrict__ row, int lo, int hi, START&& start, F&& f, ROUND&& round) {
+DASH_DEV void walk_row(const float* row, int lo, int hi, START&& start, F&& f, ROUND&& round) {
     constexpr int kTile = 4 * NT;
     const int whole = (hi - lo) / kTile;
     const int end = lo + whole * kTile, at = lo + 4 * (int)threadIdx.x;
@@ -81,7 +82,7 @@ DASH_DEV void walk_row(const float* __restrict__ row, int lo, int hi, START&& st
     if (end < hi) f(last, end + 4 * (int)threadIdx.x);
 }
 template <int DEPTH, bool STREAM, int NT = kRowThreads, class F>
-DASH_DEV void walk_row(const float* __restrict__ row, int lo, int hi, F&& f) {
+DASH_DEV void walk_row(const float* row, int lo, int hi, F&& f) {
     walk_row<DEPTH, false, STREAM, NT>(row, lo, hi, [](const f32x4_t (&)[DEPTH], int) {}, (F&&)f, [](int) { return false; });
 }
 
