@@ -244,9 +244,11 @@ def _check_distill(logits, values, indices, rest, norm=None, weight=None):
     return rows, logits.shape[1], k
 
 
-def _grad_buffer(logits: torch.Tensor, out: torch.Tensor | None, dtype: torch.dtype):
+def _grad_buffer(logits: torch.Tensor, out: torch.Tensor | None, dtype: torch.dtype | None):
     if out is None:
-        out = torch.empty(logits.shape, dtype=dtype, device=logits.device)
+        out = torch.empty(logits.shape, dtype=torch.float32 if dtype is None else dtype, device=logits.device)
+    elif dtype is not None and out.dtype != dtype:
+        raise ValueError(f"out is {out.dtype}, the gradient was asked for in {dtype}")
     if out.dtype not in (torch.float32, torch.bfloat16) or out.shape != logits.shape or out.device != logits.device or \
             (out.shape[1] > 1 and out.stride(1) != 1) or (out.shape[0] > 1 and out.stride(0) < out.shape[1]):
         raise ValueError("the gradient must be float32 or bfloat16, of the logits' shape and device, with unit column "
@@ -270,9 +272,9 @@ def distill_loss(logits: torch.Tensor, values: torch.Tensor, indices: torch.Tens
 
 def distill_grad(logits: torch.Tensor, values: torch.Tensor, indices: torch.Tensor, norm: torch.Tensor,
                  rest: torch.Tensor | None = None, temperature: float = 1.0, weight: torch.Tensor | None = None,
-                 out: torch.Tensor | None = None, dtype: torch.dtype = torch.float32) -> torch.Tensor:
+                 out: torch.Tensor | None = None, dtype: torch.dtype | None = None) -> torch.Tensor:
     """dash_distill_grad: weight[r] dloss[r]/dlogits [rows, vocab] (weight None: 1), into out (which may be the logits)
-    or a new tensor of dtype float32 or bfloat16."""
+    or a new tensor.  dtype: torch.float32 or torch.bfloat16 (None: out's, or float32); out must be of it."""
     rows, V, k = _check_distill(logits, values, indices, rest, norm, weight)
     out, code = _grad_buffer(logits, out, dtype)
     if rows:
@@ -284,9 +286,9 @@ def distill_grad(logits: torch.Tensor, values: torch.Tensor, indices: torch.Tens
 
 def distill_loss_grad(logits: torch.Tensor, values: torch.Tensor, indices: torch.Tensor,
                       rest: torch.Tensor | None = None, temperature: float = 1.0, weight: torch.Tensor | None = None,
-                      out: torch.Tensor | None = None, dtype: torch.dtype = torch.float32):
+                      out: torch.Tensor | None = None, dtype: torch.dtype | None = None):
     """dash_distill_loss_grad: (loss [rows], gradient [rows, vocab]) in one call; a row of weight 0 gets loss 0 and a
-    zero gradient."""
+    zero gradient.  out and dtype as for distill_grad."""
     rows, V, k = _check_distill(logits, values, indices, rest, weight=weight)
     out, code = _grad_buffer(logits, out, dtype)
     loss = torch.empty(rows, dtype=torch.float32, device=logits.device)
