@@ -515,7 +515,8 @@ int dash_distill_loss(const float* d_logits, int64_t ld, int32_t rows, int32_t v
  * are), of grad_dtype (DASH_F32 or DASH_BF16), = d_weight[r] dloss[r]/ds.  d_weight
  * float32 [rows] (NULL: 1).  A row of weight 0 (a padded position) gets zeros
  * whatever its logits, which are not read.  d_grad may be d_logits itself (DASH_F32 and
- * ld_grad == ld); any other overlap of the two ranges of memory is DASH_EINVAL.
+ * ld_grad == ld); any other overlap of the two ranges of memory is DASH_EINVAL, and so is a
+ * gradient whose entries lie over any other array of the call.
  */
 int dash_distill_grad(const float* d_logits, int64_t ld, int32_t rows, int32_t vocab, const float* d_t_values,
                       const int32_t* d_t_indices, const float* d_t_rest, int32_t k, float temperature,

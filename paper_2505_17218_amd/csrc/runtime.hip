@@ -10,6 +10,7 @@
 #include <cstdarg>
 #include <cstdio>
 #include <cstring>
+#include <initializer_list>
 #include <map>
 #include <mutex>
 #include <tuple>
@@ -905,13 +906,31 @@ int check_distill(const char* name, int64_t ld, int32_t rows, int32_t vocab, int
     return DASH_OK;
 }
 
-// The gradient lies over the logits exactly (float32, the same rows) or not at all.
+// Whether n bytes at p (nullable) touch the entries of rows of `row` bytes, the first at g and one every `stride` bytes.
+bool touches_rows(uintptr_t g, uintptr_t row, uintptr_t stride, int32_t rows, const void* p, size_t n) {
+    const uintptr_t lo = (uintptr_t)p, hi = lo + n;
+    if (!p || n == 0 || hi <= g || lo >= g + (uintptr_t)(rows - 1) * stride + row) return false;
+    if (lo <= g) return true;
+    const uintptr_t r = (lo - g) / stride;
+    return lo - g - r * stride < row || (r + 1 < (uintptr_t)rows && hi > g + (r + 1) * stride);
+}
+
+// The gradient lies over the logits exactly (float32, the same rows) or not at all, and over no other array of the call.
+struct Beside {
+    const void* p;  // nullable
+    size_t n;       // bytes
+    const char* what;
+};
 int check_grad(const char* name, const float* logits, int64_t ld, int32_t rows, int32_t vocab, const void* grad,
-               int64_t ld_grad, int32_t dtype) {
+               int64_t ld_grad, int32_t dtype, std::initializer_list<Beside> others) {
     if (dtype != DASH_F32 && dtype != DASH_BF16) return fail(DASH_EINVAL, "%s: bad gradient dtype %d", name, dtype);
     if (ld_grad < vocab) return fail(DASH_EINVAL, "%s: bad sizes", name);
-    if (rows == 0 || (dtype == DASH_F32 && grad == (const void*)logits && ld_grad == ld)) return DASH_OK;
+    if (rows == 0) return DASH_OK;
     const uintptr_t size = dtype == DASH_F32 ? 4 : 2, l0 = (uintptr_t)logits, g0 = (uintptr_t)grad;
+    for (const Beside& b : others)
+        if (touches_rows(g0, size * vocab, size * ld_grad, rows, b.p, b.n))
+            return fail(DASH_EINVAL, "%s: the gradient overlaps the %s", name, b.what);
+    if (dtype == DASH_F32 && grad == (const void*)logits && ld_grad == ld) return DASH_OK;
     const uintptr_t l1 = l0 + 4 * ((uintptr_t)(rows - 1) * ld + vocab), g1 = g0 + size * ((uintptr_t)(rows - 1) * ld_grad + vocab);
     if (g0 < l1 && l0 < g1) return fail(DASH_EINVAL, "%s: the gradient overlaps the logits", name);
     return DASH_OK;
@@ -1036,7 +1055,11 @@ int dash_distill_grad(const float* logits, int64_t ld, int32_t rows, int32_t voc
     if (!logits || !t_values || !t_indices || !d_norm || !d_grad)
         return fail(DASH_EINVAL, "dash_distill_grad: NULL argument");
     if (int rc = check_distill("dash_distill_grad", ld, rows, vocab, k, temperature)) return rc;
-    if (int rc = check_grad("dash_distill_grad", logits, ld, rows, vocab, d_grad, ld_grad, grad_dtype)) return rc;
+    const size_t n = rows, entries = 4 * n * k;
+    if (int rc = check_grad("dash_distill_grad", logits, ld, rows, vocab, d_grad, ld_grad, grad_dtype,
+                            {{t_values, entries, "teacher's values"}, {t_indices, entries, "teacher's indices"},
+                             {t_rest, 4 * n, "teacher's rest"}, {d_norm, 16 * n, "normalisers"}, {d_weight, 4 * n, "weights"}}))
+        return rc;
     if (rows == 0) return DASH_OK;
     DistillArgs a{logits, ld, rows, vocab, t_values, t_indices, t_rest, k, temperature, d_weight};
     a.norm = const_cast<float*>(d_norm);  // (the gradient only reads it)
@@ -1054,14 +1077,19 @@ int dash_distill_loss_grad(const float* logits, int64_t ld, int32_t rows, int32_
     if (!logits || !t_values || !t_indices || !d_loss || !d_grad)
         return fail(DASH_EINVAL, "dash_distill_loss_grad: NULL argument");
     if (int rc = check_distill("dash_distill_loss_grad", ld, rows, vocab, k, temperature)) return rc;
-    if (int rc = check_grad("dash_distill_loss_grad", logits, ld, rows, vocab, d_grad, ld_grad, grad_dtype)) return rc;
+    const size_t n = rows, entries = 4 * n * k, room = rows > 0 ? distill_workspace_bytes(rows, vocab) : 0;
+    if (int rc = check_grad("dash_distill_loss_grad", logits, ld, rows, vocab, d_grad, ld_grad, grad_dtype,
+                            {{t_values, entries, "teacher's values"}, {t_indices, entries, "teacher's indices"},
+                             {t_rest, 4 * n, "teacher's rest"}, {d_weight, 4 * n, "weights"}, {d_loss, 4 * n, "loss"},
+                             {ws, room, "workspace"}}))
+        return rc;
     if (rows == 0) return DASH_OK;
     DistillArgs a{logits, ld, rows, vocab, t_values, t_indices, t_rest, k, temperature, d_weight};
     a.loss = d_loss;
     a.grad = d_grad;
     a.ld_grad = ld_grad;
     a.grad_bf16 = grad_dtype == DASH_BF16;
-    if (int rc = check_room("dash_distill_loss_grad", ws, ws_bytes, distill_workspace_bytes(rows, vocab))) return rc;
+    if (int rc = check_room("dash_distill_loss_grad", ws, ws_bytes, room)) return rc;
     DASH_HIP(launch_distill_loss_grad(a, ws, (hipStream_t)stream));
     return DASH_OK;
 }
