@@ -142,6 +142,14 @@ def ptr(t) -> int | None:
     return t.data_ptr()
 
 
+def _i32(name: str, **sizes) -> None:
+    """Refuses sizes past 32 bits: ctypes keeps the low ones without a word, 2^32 + 5 would arrive as 5.  (Callers ask
+    first whether any is negative or past 31 bits: a call of this for each took 2 us of 18.)"""
+    for what, v in sizes.items():
+        if not -2 ** 31 <= v < 2 ** 31:
+            raise DashError(DASH_EINVAL, name, f"{what} does not fit in 32 bits")
+
+
 def i32_array(vals) -> C.Array:
     vals = [int(v) for v in vals]
     return (C.c_int32 * max(1, len(vals)))(*vals)
@@ -250,42 +258,58 @@ def dash_sample(d_logits, ld, n_rows, vocab, d_row_of, d_seq_uid, d_step, temper
 
 def dash_sample_truncated(d_logits, ld, n_rows, vocab, d_row_of, d_seq_uid, d_step, temperature, top_k, top_p, min_p,
                           seed, d_tokens_out, d_logprob_out, d_status, d_ws, ws_bytes, stream):
+    if n_rows >> 31 or vocab >> 31 or top_k >> 31:
+        _i32("dash_sample_truncated", n_rows=n_rows, vocab=vocab, top_k=top_k)
     _call("dash_sample_truncated", d_logits, ld, n_rows, vocab, d_row_of, d_seq_uid, d_step, C.c_float(temperature),
           top_k, C.c_double(top_p), C.c_double(min_p), C.c_uint64(seed), d_tokens_out, d_logprob_out, d_status,
           d_ws, ws_bytes, stream)
 
 
 def dash_sample_truncated_workspace_bytes(n_rows, vocab, top_k) -> int:
+    if n_rows >> 31 or vocab >> 31 or top_k >> 31:
+        _i32("dash_sample_truncated_workspace_bytes", n_rows=n_rows, vocab=vocab, top_k=top_k)
     return load().dash_sample_truncated_workspace_bytes(n_rows, vocab, top_k)
 
 
 def dash_top_logits_workspace_bytes(rows, vocab, k) -> int:
+    if rows >> 31 or vocab >> 31 or k >> 31:
+        _i32("dash_top_logits_workspace_bytes", rows=rows, vocab=vocab, k=k)
     return load().dash_top_logits_workspace_bytes(rows, vocab, k)
 
 
 def dash_top_logits(d_logits, ld, rows, vocab, k, temperature, d_values, d_indices, d_rest, d_ws, ws_bytes, stream):
+    if rows >> 31 or vocab >> 31 or k >> 31:
+        _i32("dash_top_logits", rows=rows, vocab=vocab, k=k)
     _call("dash_top_logits", d_logits, ld, rows, vocab, k, C.c_float(temperature), d_values, d_indices, d_rest, d_ws,
           ws_bytes, stream)
 
 
 def dash_distill_workspace_bytes(rows, vocab) -> int:
+    if rows >> 31 or vocab >> 31:
+        _i32("dash_distill_workspace_bytes", rows=rows, vocab=vocab)
     return load().dash_distill_workspace_bytes(rows, vocab)
 
 
 def dash_distill_loss(d_logits, ld, rows, vocab, d_t_values, d_t_indices, d_t_rest, k, temperature, d_loss, d_norm,
                       d_ws, ws_bytes, stream):
+    if rows >> 31 or vocab >> 31 or k >> 31:
+        _i32("dash_distill_loss", rows=rows, vocab=vocab, k=k)
     _call("dash_distill_loss", d_logits, ld, rows, vocab, d_t_values, d_t_indices, d_t_rest, k, C.c_float(temperature),
           d_loss, d_norm, d_ws, ws_bytes, stream)
 
 
 def dash_distill_grad(d_logits, ld, rows, vocab, d_t_values, d_t_indices, d_t_rest, k, temperature, d_norm, d_weight,
                       d_grad, ld_grad, grad_dtype, stream):
+    if rows >> 31 or vocab >> 31 or k >> 31:
+        _i32("dash_distill_grad", rows=rows, vocab=vocab, k=k)
     _call("dash_distill_grad", d_logits, ld, rows, vocab, d_t_values, d_t_indices, d_t_rest, k, C.c_float(temperature),
           d_norm, d_weight, d_grad, ld_grad, grad_dtype, stream)
 
 
 def dash_distill_loss_grad(d_logits, ld, rows, vocab, d_t_values, d_t_indices, d_t_rest, k, temperature, d_weight,
                            d_loss, d_grad, ld_grad, grad_dtype, d_ws, ws_bytes, stream):
+    if rows >> 31 or vocab >> 31 or k >> 31:
+        _i32("dash_distill_loss_grad", rows=rows, vocab=vocab, k=k)
     _call("dash_distill_loss_grad", d_logits, ld, rows, vocab, d_t_values, d_t_indices, d_t_rest, k,
           C.c_float(temperature), d_weight, d_loss, d_grad, ld_grad, grad_dtype, d_ws, ws_bytes, stream)
 

@@ -84,3 +84,25 @@ def test_engine_refuses_a_gradient_over_what_it_reads():
         assert torch.equal(engine.distill_grad(logits, values, indices, norm, weight=weight, out=wide), want)
         assert torch.equal(engine.distill_loss_grad(logits, values, indices, weight=weight, out=wide)[1], want)
         assert (weight == 1).all()
+
+
+@pytest.mark.skipif(not os.path.exists(L.LIB_PATH), reason="libdash.so not built")
+@pytest.mark.parametrize("name", ["n", "vocab", "k"])
+@pytest.mark.parametrize("f", [
+    lambda n=4, vocab=64, k=5: L.dash_sample_truncated(0x10000000, 1 << 40, n, vocab, None, 0x2000, 0x3000, 1.0, k, 0.9, 0.0, 1,
+                                                       0x4000, None, None, 0x10000, 1 << 40, None),
+    lambda n=4, vocab=64, k=5: L.dash_sample_truncated_workspace_bytes(n, vocab, k),
+    lambda n=4, vocab=64, k=5: L.dash_top_logits(0x10000000, 1 << 40, n, vocab, k, 1.0, 0x2000, 0x3000, None, 0x10000, 1 << 40,
+                                                 None),
+    lambda n=4, vocab=64, k=5: L.dash_top_logits_workspace_bytes(n, vocab, k),
+    lambda n=4, vocab=64, k=5: L.dash_distill_loss(0x10000000, 1 << 40, n, vocab, 0x2000, 0x3000, None, k, 1.0, 0x4000, 0x5000,
+                                                   0x10000, 1 << 40, None),
+    lambda n=4, vocab=64, k=5: L.dash_distill_grad(0x10000000, 1 << 40, n, vocab, 0x2000, 0x3000, None, k, 1.0, 0x5000, None,
+                                                   1 << 50, 1 << 40, L.DASH_F32, None),
+    lambda n=4, vocab=64, k=5: L.dash_distill_loss_grad(0x10000000, 1 << 40, n, vocab, 0x2000, 0x3000, None, k, 1.0, None,
+                                                        0x4000, 1 << 50, 1 << 40, L.DASH_F32, 0x10000, 1 << 40, None)])
+def test_sizes_past_32_bits_do_not_wrap(f, name):
+    for big in (2 ** 32, 2 ** 32 + 5, 2 ** 31, -2 ** 31 - 1, 2 ** 63 - 1):
+        with pytest.raises(L.DashError) as e:
+            f(**{name: big})
+        assert e.value.status == L.DASH_EINVAL and "32 bits" in str(e.value)
