@@ -496,7 +496,7 @@ int dash_top_logits(const float* d_logits, int64_t ld, int32_t rows, int32_t voc
  * An index may occur once in a row; a row in which one occurs twice gives NaN.
  * d_t_rest float32 [rows] as dash_top_logits writes it at the same T; NULL means
  * -inf: the teacher's entries renormalised over themselves.  A teacher without any mass
- * gives loss 0 and a zero gradient.  A -inf student logit has probability zero (loss
+ * gives loss 0 and a zero gradient, whatever its indices and the student.  A -inf student logit has probability zero (loss
  * +inf where the teacher gives it mass); a student row with NaN, +inf or
  * no finite logit gives NaN.  Sums are float32 terms in float64 and float64 for the teacher's
  * tokens; results do not depend on scheduling.

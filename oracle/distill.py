@@ -42,14 +42,14 @@ def row(s: np.ndarray, values: np.ndarray, indices: np.ndarray, rest: float | No
     indices = np.asarray(indices, np.int64)
     known = (indices >= 0) & (indices < V)
     at = indices[known]
-    if np.unique(at).size != at.size:
-        nan = np.full(V, np.nan)
-        return Row(math.nan, nan, nan, math.nan, nan, math.nan)
     t = np.where(known, np.asarray(values, np.float64) / T, -np.inf)
     outcomes = np.append(t, -np.inf if rest is None else float(rest))
     m, z = _exp_sum(outcomes)
     if z == 0.0:  # the row has no teacher
         return Row(0.0, np.zeros(V), np.zeros(t.size), 0.0, np.exp(s - s.max()), 0.0)
+    if np.unique(at).size != at.size:
+        nan = np.full(V, np.nan)
+        return Row(math.nan, nan, nan, math.nan, nan, math.nan)
     lp = outcomes - m - math.log(z)
     p = np.exp(lp)
     if not np.isfinite(s).any() or np.isnan(s).any() or (s == np.inf).any():
