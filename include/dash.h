@@ -320,9 +320,10 @@ int dash_sample(const float* d_logits, int64_t ld, int32_t n_rows, int32_t vocab
 
 /*
  * Truncated sampling: dash_sample over the tokens that top_k, top_p and min_p
- * keep.  (The paper draws from the whole softmax; this is for serving a policy,
- * and for rollouts that leave its tail out.)  Order a row's finite logits
- * descending, equal ones by ascending index, and let w_v = exp((l_v - l_max) / T).
+ * keep.  (The paper draws from the whole softmax, and so does dash_rollout; this is for
+ * serving a policy from the rows that dash_prefill and dash_decode_step hand out.)  Order a
+ * row's finite logits descending, equal ones by ascending index, and let
+ * w_v = exp((l_v - l_max) / T).
  * A token is kept iff
  *   - fewer than top_k tokens come before it in the order (top_k = 0: all),
  *   - the w of the tokens before it sum to less than top_p times the sum over
@@ -474,7 +475,9 @@ int dash_logits_kl(const float* d_theta, const float* d_base, int64_t ld, int32_
  * exp(l_v / T) over the row's other finite logits (-inf if there are none).
  * DASH_EINVAL if k < 1, temperature <= 0 or not finite, vocab < 1 or > 2^28, or
  * ld < vocab; DASH_ENOTSUP if k > 1024 or for more than 2^21 rows.  d_ws as for
- * dash_sample_truncated, dash_top_logits_workspace_bytes(rows, vocab, k) bytes.
+ * dash_sample_truncated, dash_top_logits_workspace_bytes(rows, vocab, k) bytes: a list of the entries
+ * above a sampled bound per row, with 2048 rows of 151,936 34 MB for k = 64 and 268 MB, a
+ * fifth of the logits, for k = 500 and above (dash_sample_truncated with top_k likewise).
  */
 size_t dash_top_logits_workspace_bytes(int32_t rows, int32_t vocab, int32_t k);
 int dash_top_logits(const float* d_logits, int64_t ld, int32_t rows, int32_t vocab, int32_t k, float temperature,
@@ -496,10 +499,10 @@ int dash_top_logits(const float* d_logits, int64_t ld, int32_t rows, int32_t voc
  * An index may occur once in a row; a row in which one occurs twice gives NaN.
  * d_t_rest float32 [rows] as dash_top_logits writes it at the same T; NULL means
  * -inf: the teacher's entries renormalised over themselves.  A teacher without any mass
- * gives loss 0 and a zero gradient, whatever its indices and the student.  A -inf student logit has probability zero (loss
- * +inf where the teacher gives it mass); a student row with NaN, +inf or
- * no finite logit gives NaN.  Sums are float32 terms in float64 and float64 for the teacher's
- * tokens; results do not depend on scheduling.
+ * gives loss 0 and a zero gradient, whatever its indices and the student.  A -inf student
+ * logit has probability zero (loss +inf where the teacher gives it mass); a student row with
+ * NaN, +inf or no finite logit gives NaN.  Sums are float32 terms in float64 and float64 for
+ * the teacher's tokens; results do not depend on scheduling.
  * d_norm float32 [rows, 4]: normalisers of the row, for dash_distill_grad with the same
  * logits, teacher and T.
  * DASH_EINVAL and DASH_ENOTSUP as for dash_top_logits.  d_ws as for dash_sample_truncated,

@@ -456,7 +456,9 @@ distill_loss_grad_k(DistillArgs a) {
     store_tokens(grad, t, g, 0, a.vocab);
 }
 
-// Rows are cut where there are fewer of them than work-groups that fill the GPU.
+// Rows are cut where there are fewer of them than work-groups that fill the GPU.  From 513 on they are whole, with the
+// first loads and the float64 sums at the end exposed once: 512 rows of 50,257 27 us, 513 30, 701 33, 1024 43; of
+// 151,936 56, 67, 76, 102.
 RowSplit loss_split(int rows, int vocab) {
     return split_row(vocab, std::min({64, kDistillTarget / std::max(rows, 1), vocab / kDistillStretch}));
 }
@@ -465,6 +467,9 @@ RowSplit loss_split(int rows, int vocab) {
 // LDS at once, and what is not read again outweighs that a CU has one work-group instead of
 // four.  2048 rows, pair of launches / one: 32,768 entries 159 / 164 us in float32 and 133 / 159 in bf16,
 // 50,257 263 / 237 and 216 / 216, 80,000 360 / 311 and 293 / 282, 151,936 721 / 545 and 556 / 438; 706 47 / 87.
+// Fewer rows, in float32: 513 of 50,257 79 / 82, 600 91 / 86, 769 111 / 112, 1024 136 / 125; 513 of 151,936 205 / 172,
+// 769 279 / 232, in bf16 174 / 149 and 229 / 201.  So a round of 256 work-groups that is begun costs the one launch
+// 4% at most.
 bool fused(int rows, int vocab, bool bf16) {
     return loss_split(rows, vocab).n == 1 && vocab >= (bf16 ? 1 << 16 : 40960) && vocab <= kStretch;
 }

@@ -103,7 +103,7 @@ inline RowSplit split_row(int vocab, int n) {
 // difference and log2(e) / T, bit for bit.
 DASH_DEV float half_gap(float x, float half) { return __builtin_fmaf(x, 0.5f, -half); }
 // 2 log2(e) / T, so that e^((x - m) / T) = 2^(half_gap(x, m / 2) scale); finite for every T > 0 (0 times it
-// stays 0).
+// stays 0): below T = 8.5e-39, where logits less than 1e-36 apart would matter, it is that of 8.5e-39.
 __host__ __device__ inline float exp2_scale(double temperature) {
     return (float)fmin(2.0 * 1.4426950408889634 / temperature, (double)FLT_MAX);
 }

@@ -259,7 +259,10 @@ def _grad_buffer(logits: torch.Tensor, out: torch.Tensor | None, dtype: torch.dt
 def distill_loss(logits: torch.Tensor, values: torch.Tensor, indices: torch.Tensor, rest: torch.Tensor | None = None,
                  temperature: float = 1.0):
     """dash_distill_loss against a teacher's entries as top_logits gives them (rest None: renormalised over the
-    entries): (float32 loss [rows], float32 normalisers [rows, 4] for distill_grad)."""
+    entries): (float32 loss [rows], float32 normalisers [rows, 4] for distill_grad).
+
+    No autograd graph is built, here and in distill_grad and distill_loss_grad: logits that require a gradient are read
+    as they are, and what the gradient functions return is handed on by the caller, logits.backward(gradient)."""
     rows, V, k = _check_distill(logits, values, indices, rest)
     loss = torch.empty(rows, dtype=torch.float32, device=logits.device)
     norm = torch.empty(rows, 4, dtype=torch.float32, device=logits.device)
@@ -274,7 +277,8 @@ def distill_grad(logits: torch.Tensor, values: torch.Tensor, indices: torch.Tens
                  rest: torch.Tensor | None = None, temperature: float = 1.0, weight: torch.Tensor | None = None,
                  out: torch.Tensor | None = None, dtype: torch.dtype | None = None) -> torch.Tensor:
     """dash_distill_grad: weight[r] dloss[r]/dlogits [rows, vocab] (weight None: 1), into out (which may be the logits)
-    or a new tensor.  dtype: torch.float32 or torch.bfloat16 (None: out's, or float32); out must be of it."""
+    or a new tensor.  dtype: torch.float32 or torch.bfloat16 (None: out's, or float32); out must be of it, and may lie
+    over no other argument."""
     rows, V, k = _check_distill(logits, values, indices, rest, norm, weight)
     out, code = _grad_buffer(logits, out, dtype)
     if rows:
