@@ -634,6 +634,20 @@ draw_last(Draw a, int rows, RowState* __restrict__ state, int* __restrict__ open
                     if (fabs(before - a.top_p * w.z) <= kMassTol * w.z) kept = kept_exactly(a, row, w.l, w.tok, w.top, red_d);
                 }
                 if (kept || next == kNone) break;  // (the first token of the order is kept: there is a next one)
+                if constexpr (LAST && !UNIT_T) {
+                    // A winner whose quotient overflows has no noise: the draws go down the row index by index, as many
+                    // passes as there are such logits in ascending order.  The largest one's quotient overflows with it, any
+                    // other logit is 2^103 T below that and without mass, so what is kept is among the entries equal
+                    // to the largest, and the first of these is drawn.
+                    if (fabsf(div_rn(w.l, a.temperature)) == INFINITY) {
+                        w.l = value_below(top_key(w.top));
+                        w.tok = 0;
+                        draw_before<kLater, UNIT_T>(a, b, row, 0, a.vocab, w, &floor_s, best, red_d, s, next);
+                        w.tok = next;
+                        w.l = row[next];
+                        break;
+                    }
+                }
                 w.tok = next;
                 w.l = row[next];
                 if (a.top_p >= 1.0 || kept_by_own_mass(a, w.l, w.top, w.z)) break;

@@ -108,3 +108,19 @@ def test_weights_over_the_temperature_past_the_float_range(T, weight, rows, V):
         np.testing.assert_array_equal(got[past], np.sign(want.grad[past]) * np.inf)
         want.grad[past] = got[past] = 0.0
         _check_grad(got, want, T, float(w[at[r]]), torch.float32, (r, V, T))
+
+
+@pytest.mark.parametrize("rows, V", [(4, 3001), (4, 20001), (300, 9001)])
+@pytest.mark.parametrize("T, low, high", [(1e-38, 4.0, 9.0), (1e-30, 1e9, 2e9), (0.5, 2e38, 3.3e38), (0.5, -3.3e38, -2e38)])
+def test_ascending_rows_whose_quotients_overflow(T, low, high, rows, V):
+    """Every score is infinite, so a draw takes the lowest index: down an ascending row one entry at a time, if each pass
+    leaves out only what came before.  The largest logits are equal; rows cut, uncut and in two rounds."""
+    require_gpu()
+    rng = np.random.default_rng([37, V])
+    l = np.sort(rng.uniform(low, high, (4, V)).astype(np.float32), axis=1)
+    assert (np.abs(l.astype(np.float64) / T) > 2.0 ** 128).all()
+    l[0, -5:] = l[0, -1]
+    l[1, V // 3] = l[1, -1]
+    l[2, ::7] = -np.inf
+    for top_p, min_p in ((0.9, 0.0), (0.3, 0.0), (0.5, 0.1), (1.0, 0.2)):
+        _check_sample(l, T, 0, top_p, min_p, row_of=np.arange(rows) % 4)
